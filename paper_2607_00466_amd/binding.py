@@ -21,6 +21,7 @@ INCLUDE_DIR = os.path.join(os.path.dirname(_PKG), "include")
 HEADER_PATH = os.path.join(INCLUDE_DIR, "eldr_moe.h")
 HEADER_PATHS = (HEADER_PATH, os.path.join(INCLUDE_DIR, "eldr_signature.h"),
                 os.path.join(INCLUDE_DIR, "eldr_calibration.h"),
+                os.path.join(INCLUDE_DIR, "eldr_attention.h"),
                 os.path.join(INCLUDE_DIR, "eldr_route.h"))
 
 MOE_OK = 0
@@ -43,6 +44,14 @@ class MoeDims(ctypes.Structure):
 
     def __repr__(self) -> str:
         return f"MoeDims(T={self.T}, H={self.H}, E={self.E}, K={self.K}, I={self.I})"
+
+
+class AttnDims(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("R", "Hq", "Hkv", "D", "block_size", "max_blocks",
+                                              "num_blocks", "kv_type")] + [("block_stride", ctypes.c_int64)]
+
+    def __repr__(self) -> str:
+        return "AttnDims(" + ", ".join(f"{n}={getattr(self, n)}" for n, _ in self._fields_) + ")"
 
 
 class MoeError(RuntimeError):
@@ -86,6 +95,13 @@ _SIGNATURES = {
     "moe_sig_capture": (ctypes.c_int, [_vp, _vp] + [ctypes.c_int32] * 7 + [_vp, _vp, _vp]),
     "moe_sig_reset": (ctypes.c_int, [_vp] + [ctypes.c_int32] * 4 + [_vp, _vp]),
     "moe_sig_request_counts": (ctypes.c_int, [_vp, _vp, _vp] + [ctypes.c_int32] * 5 + [_vp, _vp]),
+    "moe_kv_append": (ctypes.c_int, [_vp] * 3 + [ctypes.c_int64] * 3 + [ctypes.c_int32] * 2 + [_vp, ctypes.c_int32] +
+                      [_vp] * 3 + [ctypes.c_int32] * 3 + [_vp, AttnDims] + [_vp] * 6),
+    "moe_attn_workspace_bytes": (ctypes.c_size_t, [AttnDims]),
+    "moe_attn_decode": (ctypes.c_int, [_vp] * 7 + [ctypes.c_int32] + [_vp] * 3 + [ctypes.c_int32, ctypes.c_float, AttnDims] +
+                        [_vp] * 3 + [ctypes.c_size_t, _vp]),
+    "moe_attn_weights": (ctypes.c_int, [_vp] * 6 + [ctypes.c_int32, _vp, ctypes.c_float, _vp, AttnDims] + [_vp] * 3),
+    "moe_kv_evict": (ctypes.c_int, [_vp] * 6 + [AttnDims, ctypes.c_int32, ctypes.c_int32] + [_vp] * 7),
     "moe_stream_read_probe": (ctypes.c_int, [_vp, ctypes.c_size_t, _vp, _vp]),
     "eldr_idf": (ctypes.c_int, [_vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _vp]),
     "eldr_signature": (ctypes.c_int, [_vp, _vp, ctypes.c_int32, ctypes.c_int32, _vp,
@@ -657,6 +673,189 @@ def moe_sig_request_counts(sig, block_table, n_blocks, out=None, stream=None) ->
         _ptr(sig), _ptr(block_table), _ptr(n_blocks), R, max_blocks, L, E, nb, _ptr(out),
         _stream(stream)))
     return out
+
+
+# ----------------------------------------------------------------------------- attention over the paged cache
+#
+# Caches are tensors whose first four dimensions are [num_blocks, Hkv,
+# block_size, D], of torch.bfloat16 or torch.float8_e4m3fn; only the block
+# stride may be larger than dense (d.block_stride), as where keys and values
+# interleave in one allocation.
+
+MOE_KV_BF16, MOE_KV_FP8 = 0, 1
+MOE_IN_BF16, MOE_IN_FP32 = 0, 1
+_KV_TYPES = {torch.bfloat16: MOE_KV_BF16, torch.float8_e4m3fn: MOE_KV_FP8}
+_KV_DTYPES = (torch.bfloat16, torch.float8_e4m3fn)
+_IN_TYPES = {torch.bfloat16: MOE_IN_BF16, torch.float32: MOE_IN_FP32}
+
+
+def attn_dims(R: int, Hq: int, Hkv: int, D: int, block_size: int, max_blocks: int, num_blocks: int,
+              kv_dtype=torch.bfloat16, block_stride: int = 0) -> AttnDims:
+    """The shape of one attention layer: R requests, Hq query heads over Hkv kv
+    heads of D values, pages of block_size slots, block tables [R, max_blocks]
+    into num_blocks pages of kv_dtype."""
+    if kv_dtype not in _KV_TYPES:
+        raise ValueError(f"kv_dtype: expected torch.bfloat16 or torch.float8_e4m3fn, got {kv_dtype}")
+    return AttnDims(R, Hq, Hkv, D, block_size, max_blocks, num_blocks, _KV_TYPES[kv_dtype], block_stride)
+
+
+def _need_cache(t: torch.Tensor, name: str, d: AttnDims) -> None:
+    dense = d.Hkv * d.block_size * d.D
+    if (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is _KV_DTYPES[d.kv_type]
+            and t.shape == (d.num_blocks, d.Hkv, d.block_size, d.D)
+            and (t.is_contiguous() if d.block_stride in (0, dense)
+                 else t.stride() == (d.block_stride, d.block_size * d.D, d.D, 1) or t.numel() == 0)):
+        return
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name}: must be a device tensor, got {t.device}")
+    if t.dtype != _KV_DTYPES[d.kv_type]:
+        raise ValueError(f"{name}: expected {_KV_DTYPES[d.kv_type]}, got {t.dtype}")
+    raise ValueError(f"{name}: expected {(d.num_blocks, d.Hkv, d.block_size, d.D)} with a block stride of "
+                     f"{d.block_stride or dense}, got {tuple(t.shape)} with strides {t.stride()}")
+
+
+def _need_opt(t, name: str, dtype: torch.dtype, numel: int) -> None:
+    if t is not None:
+        _need(t, name, dtype, numel)
+
+
+def _need_rows(t: torch.Tensor, name: str, T: int, heads: int, D: int) -> int:
+    """A [T, heads, D] tensor whose heads and values are contiguous; its token stride."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name}: must be a device tensor, got {t.device}")
+    if t.shape != (T, heads, D):
+        raise ValueError(f"{name}: expected [{T}, {heads}, {D}], got {tuple(t.shape)}")
+    token, head, value = t.stride()
+    if (D > 1 and value != 1) or (heads > 1 and head != D):
+        raise ValueError(f"{name}: heads and values must be contiguous, got strides {t.stride()}")
+    return token if T > 1 else heads * D  # one row has no stride
+
+
+def _need_groups(group_start, prefix_len) -> int:
+    if (group_start is None) != (prefix_len is None):
+        raise ValueError("group_start and prefix_len come together")
+    if group_start is None:
+        return 0
+    n = prefix_len.numel()
+    _need(prefix_len, "prefix_len", torch.int32, n)
+    _need(group_start, "group_start", torch.int32, n + 1)
+    return n
+
+
+def moe_kv_append(q, k, v, positions, pair_axis, cos, sin, slots, d: AttnDims, q_out, k_cache, v_cache,
+                  k_scale=None, v_scale=None, interleaved: bool = False, stream=None) -> None:
+    """Rotate q [T, Hq, D] into q_out and k [T, Hkv, D] by positions [n_axes, T], and
+    store k and v in the caches' slots.  q, k and v may be views of one projection's
+    rows; q and q_out may be None where only keys and values are wanted."""
+    T = slots.numel()
+    if positions.dim() != 2 or positions.shape[1] != T:
+        raise ValueError(f"positions: expected [n_axes, {T}]")
+    if cos.dim() != 2 or cos.shape != sin.shape:
+        raise ValueError("cos, sin: expected two [max_pos, rot / 2] tensors")
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out come together")
+    n_axes, (max_pos, half) = positions.shape[0], cos.shape
+    if pair_axis.numel() != half:
+        raise ValueError(f"pair_axis: expected {half} axes, one a pair")
+    q_stride = 0
+    if q is not None:
+        q_stride = _need_rows(q, "q", T, d.Hq, d.D)
+        _need(q_out, "q_out", torch.bfloat16, T * d.Hq * d.D)
+    k_stride, v_stride = _need_rows(k, "k", T, d.Hkv, d.D), _need_rows(v, "v", T, d.Hkv, d.D)
+    if k.dtype not in _IN_TYPES or v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
+        raise ValueError("q, k and v: expected all torch.bfloat16 or all torch.float32")
+    _need(positions, "positions", torch.int32, n_axes * T)
+    _need(pair_axis, "pair_axis", torch.int32, half)
+    _need(cos, "cos", torch.float32, max_pos * half)
+    _need(sin, "sin", torch.float32, max_pos * half)
+    _need(slots, "slots", torch.int32, T)
+    _need_opt(k_scale, "k_scale", torch.float32, d.Hkv)
+    _need_opt(v_scale, "v_scale", torch.float32, d.Hkv)
+    _need_cache(k_cache, "k_cache", d)
+    _need_cache(v_cache, "v_cache", d)
+    _check("moe_kv_append", load().moe_kv_append(
+        _ptr(q), _ptr(k), _ptr(v), q_stride, k_stride, v_stride, _IN_TYPES[k.dtype], T, _ptr(positions), n_axes,
+        _ptr(pair_axis), _ptr(cos), _ptr(sin), max_pos, 2 * half, int(bool(interleaved)), _ptr(slots), d,
+        _ptr(k_scale), _ptr(v_scale), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _stream(stream)))
+
+
+def moe_attn_workspace_bytes(d: AttnDims) -> int:
+    return int(load().moe_attn_workspace_bytes(d))
+
+
+def attn_workspace(d: AttnDims, device="cuda") -> torch.Tensor:
+    """A workspace for moe_attn_decode (allocated once, for every layer on a stream)."""
+    return torch.zeros(max(16, moe_attn_workspace_bytes(d)) // 4, dtype=torch.float32, device=device)
+
+
+def moe_attn_decode(q, k_cache, v_cache, block_table, lens, d: AttnDims, out, lse, ws, group_start=None,
+                    prefix_len=None, k_scale=None, v_scale=None, sinks=None, window: int = 0, scale=None,
+                    stream=None) -> None:
+    """Attention of one query token a request, q [R, Hq, D], over its cached tokens;
+    out [R, Hq, D], lse [R, Hq] or None.  scale defaults to 1 / sqrt(D)."""
+    n = d.R * d.Hq
+    _need(q, "q", torch.bfloat16, n * d.D)
+    _need(out, "out", torch.bfloat16, n * d.D)
+    _need_opt(lse, "lse", torch.float32, n)
+    _need_cache(k_cache, "k_cache", d)
+    _need_cache(v_cache, "v_cache", d)
+    _need(block_table, "block_table", torch.int32, d.R * d.max_blocks)
+    _need(lens, "lens", torch.int32, d.R)
+    groups = _need_groups(group_start, prefix_len)
+    _need_opt(k_scale, "k_scale", torch.float32, d.Hkv)
+    _need_opt(v_scale, "v_scale", torch.float32, d.Hkv)
+    _need_opt(sinks, "sinks", torch.float32, d.Hq)
+    ws_bytes = _need_ws(ws, d)
+    _check("moe_attn_decode", load().moe_attn_decode(
+        _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(lens), _ptr(group_start), _ptr(prefix_len),
+        groups, _ptr(k_scale), _ptr(v_scale), _ptr(sinks), window, d.D ** -0.5 if scale is None else scale, d,
+        _ptr(out), _ptr(lse), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def moe_attn_weights(q, k_cache, block_table, lens, lse, d: AttnDims, weights_in, weights_out, group_start=None,
+                     prefix_len=None, k_scale=None, scale=None, stream=None) -> None:
+    """weights_out [R, Hkv, max_blocks * block_size] = weights_in (None: zeros) plus the
+    attention weight that each cached token received; lse from moe_attn_decode."""
+    n, rows = d.R * d.Hq, d.R * d.Hkv * d.max_blocks * d.block_size
+    _need(q, "q", torch.bfloat16, n * d.D)
+    _need(lse, "lse", torch.float32, n)
+    _need_cache(k_cache, "k_cache", d)
+    _need(block_table, "block_table", torch.int32, d.R * d.max_blocks)
+    _need(lens, "lens", torch.int32, d.R)
+    groups = _need_groups(group_start, prefix_len)
+    _need_opt(k_scale, "k_scale", torch.float32, d.Hkv)
+    _need_opt(weights_in, "weights_in", torch.float32, rows)
+    _need(weights_out, "weights_out", torch.float32, rows)
+    _check("moe_attn_weights", load().moe_attn_weights(
+        _ptr(q), _ptr(k_cache), _ptr(block_table), _ptr(lens), _ptr(group_start), _ptr(prefix_len), groups,
+        _ptr(k_scale), d.D ** -0.5 if scale is None else scale, _ptr(lse), d, _ptr(weights_in), _ptr(weights_out),
+        _stream(stream)))
+
+
+def moe_kv_evict(weights, pos, lens, seen, block_table, d: AttnDims, budget: int, recent: int, k_cache, v_cache, src,
+                 new_lens, weights_out, pos_out, protect=None, stream=None) -> None:
+    """Cut every request to its `budget` cached tokens of largest weight, in place
+    (see include/eldr_attention.h for the order and for what moves)."""
+    rows = d.R * d.Hkv * d.max_blocks * d.block_size
+    _need(weights, "weights", torch.float32, rows)
+    _need(pos, "pos", torch.int32, rows)
+    _need(lens, "lens", torch.int32, d.R)
+    _need(seen, "seen", torch.int32, d.R)
+    _need_opt(protect, "protect", torch.int32, d.R)
+    _need(block_table, "block_table", torch.int32, d.R * d.max_blocks)
+    _need_cache(k_cache, "k_cache", d)
+    _need_cache(v_cache, "v_cache", d)
+    _need(src, "src", torch.int32, d.R * d.Hkv * budget)
+    _need(new_lens, "new_lens", torch.int32, d.R)
+    _need(weights_out, "weights_out", torch.float32, rows)
+    _need(pos_out, "pos_out", torch.int32, rows)
+    _check("moe_kv_evict", load().moe_kv_evict(
+        _ptr(weights), _ptr(pos), _ptr(lens), _ptr(seen), _ptr(protect), _ptr(block_table), d, budget, recent,
+        _ptr(k_cache), _ptr(v_cache), _ptr(src), _ptr(new_lens), _ptr(weights_out), _ptr(pos_out), _stream(stream)))
 
 
 # ----------------------------------------------------------------------------- calibration

@@ -1,0 +1,76 @@
+// What the attention kernels share: the paged cache's addresses, its two value
+// types, and the host's checks of moe_attn_dims.
+#pragma once
+
+#include "common.hpp"
+#include "eldr_attention.h"
+
+namespace eldr {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// The kernels' view of one cache: pages of block_size = 1 << shift slots.
+struct Pages {
+  const int32_t* table;  // [R, max_blocks]
+  int64_t block_stride;  // elements
+  int32_t shift, max_blocks, num_blocks, Hkv, D;
+
+  // Slots a request can have.
+  __device__ __forceinline__ int capacity() const { return max_blocks << shift; }
+  // The page of slot j of request r; outside [0, num_blocks) where it is absent.
+  __device__ __forceinline__ int page(int r, int j) const {
+    return table[(int64_t)r * max_blocks + (j >> shift)];
+  }
+  __device__ __forceinline__ bool has(int b) const { return (uint32_t)b < (uint32_t)num_blocks; }
+  // Element offset of slot j's row of kv head h in page b.
+  __device__ __forceinline__ int64_t row(int b, int h, int j) const {
+    return (int64_t)b * block_stride + (int64_t)((h << shift) + (j & ((1 << shift) - 1))) * D;
+  }
+};
+
+__device__ __forceinline__ float bf16_to_float(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+
+// Round to nearest even; two values in one word, the first in the low half.
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 v = {(__bf16)lo, (__bf16)hi};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+}  // namespace eldr
+
+namespace eldr_host {
+
+inline bool power_of_two(int32_t v) { return v > 0 && (v & (v - 1)) == 0; }
+
+// The shape that every attention call shares.
+inline int check_attn_dims(const moe_attn_dims& d) {
+  if (d.R < 0 || d.Hq <= 0 || d.Hkv <= 0 || d.D <= 0 || d.block_size <= 0 || d.max_blocks < 0 ||
+      d.num_blocks < 0 || d.block_stride < 0 || d.Hq % d.Hkv != 0)
+    return MOE_ERR_INVALID;
+  if (d.kv_type != MOE_KV_BF16 && d.kv_type != MOE_KV_FP8) return MOE_ERR_INVALID;
+  const int64_t dense = (int64_t)d.Hkv * d.block_size * d.D;
+  if (d.block_stride != 0 && d.block_stride < dense) return MOE_ERR_INVALID;
+  if (d.R > MOE_ATTN_MAX_R || d.Hq > MOE_ATTN_MAX_HEADS) return MOE_ERR_UNSUPPORTED;
+  if (d.D != 64 && d.D != 128 && d.D != 256) return MOE_ERR_UNSUPPORTED;
+  if (!power_of_two(d.block_size) || d.block_size < MOE_ATTN_MIN_BLOCK || d.block_size > MOE_ATTN_MAX_BLOCK)
+    return MOE_ERR_UNSUPPORTED;
+  if ((int64_t)d.max_blocks * d.block_size > MOE_ATTN_MAX_TOKENS) return MOE_ERR_UNSUPPORTED;
+  // rows start at multiples of 16 bytes
+  if (d.block_stride % 16 != 0) return MOE_ERR_UNSUPPORTED;
+  return MOE_OK;
+}
+
+inline eldr::Pages pages_of(const moe_attn_dims& d, const int32_t* table) {
+  eldr::Pages p;
+  p.table = table;
+  p.block_stride = d.block_stride ? d.block_stride : (int64_t)d.Hkv * d.block_size * d.D;
+  p.shift = __builtin_ctz((unsigned)d.block_size);
+  p.max_blocks = d.max_blocks;
+  p.num_blocks = d.num_blocks;
+  p.Hkv = d.Hkv;
+  p.D = d.D;
+  return p;
+}
+
+}  // namespace eldr_host
