@@ -78,7 +78,7 @@ extern "C" {
 /* Limits.  D is 64, 128 or 256; Hkv divides Hq; block_size is a power of two. */
 #define MOE_ATTN_MAX_R 1024
 #define MOE_ATTN_MAX_HEADS 256
-#define MOE_ATTN_MIN_BLOCK 8
+#define MOE_ATTN_MIN_BLOCK 16
 #define MOE_ATTN_MAX_BLOCK 1024
 #define MOE_ATTN_MAX_TOKENS (1 << 19) /* max_blocks * block_size */
 #define MOE_ATTN_MAX_APPEND (1 << 20)

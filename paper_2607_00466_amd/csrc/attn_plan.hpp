@@ -1,0 +1,151 @@
+// How a batch's attention is cut into work: what each request shares, and two
+// lines of equal units that are dealt to the workgroups in equal stretches.
+//
+// A request's cached slots are [0, reach), read with its group, and
+// [max(reach, lens - window), lens), its own.  Every workgroup works the plan
+// out for itself from lens and the groups (a few thousand cycles, no launch of
+// its own, and no host copy of the lengths, so that a graph can replay a step
+// while the lengths grow).
+//
+//   own line     for each head tile, for each request: tiles of kTile slots
+//   shared line  for each kv head, for each group, for each row tile: tiles
+#pragma once
+
+#include "attn_common.hpp"
+
+namespace eldr {
+
+constexpr int kTile = 128;  // slots of a unit; tiles start at multiples of it
+
+struct Groups {
+  const int32_t *lens, *start, *prefix;
+  int32_t R, n, window;  // n: groups (0 where a window forbids sharing)
+};
+
+// The plan in LDS.
+struct Plan {
+  int *own;     // [R + 1] own tiles before each request
+  int *reach;   // [R] slots read with the group
+  int *group;   // [R] the request's group, -1: none
+  int *shared;  // [n + 1] shared units (row tiles x slot tiles) before each group
+  int *least;   // [n] slots the group shares
+
+  static __host__ __device__ size_t bytes(int R, int n) { return sizeof(int) * (3 * (size_t)R + 1 + 2 * (size_t)n + 1); }
+};
+
+// Inclusive sum over a wave's lanes.
+__device__ __forceinline__ int wave_sum_before(int v) {
+  const int lane = threadIdx.x % kWave;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int y = __shfl_up(v, o);
+    if (lane >= o) v += y;
+  }
+  return v;
+}
+
+// out[0] = 0, out[i + 1] = sum of f(0 .. i), by THREADS threads, i ascending a thread.
+template <int THREADS, typename F>
+__device__ __forceinline__ void sums(int n, int* out, int* waves, F f) {
+  const int t = threadIdx.x, lane = t % kWave, wave = t / kWave;
+  const int per = (n + THREADS - 1) / THREADS;
+  int mine = 0;
+  for (int i = t * per; i < min(n, t * per + per); ++i) mine += f(i);
+  const int upto = wave_sum_before(mine);
+  if (lane == kWave - 1) waves[wave] = upto;
+  __syncthreads();
+  int at = upto - mine;
+#pragma unroll
+  for (int w = 0; w < THREADS / kWave; ++w) at += w < wave ? waves[w] : 0;
+  if (t == 0) out[0] = 0;
+  for (int i = t * per; i < min(n, t * per + per); ++i) {
+    at += f(i);
+    out[i + 1] = at;
+  }
+  __syncthreads();
+}
+
+__device__ __forceinline__ int tiles_of(int lo, int hi) {
+  return hi > lo ? (hi + kTile - 1) / kTile - lo / kTile : 0;
+}
+
+__device__ __forceinline__ int clamp_len(int n, int capacity) { return min(max(n, 0), capacity); }
+
+// First slot of a request's own part.
+__device__ __forceinline__ int own_from(int n, int reach, int window) {
+  return window > 0 ? max(0, n - window) : min(reach, n);
+}
+
+// Works the plan out.  `lds`: Plan::bytes of LDS; `waves`: THREADS / 64 ints of
+// LDS; G: query heads a kv head; row_tile: rows of a shared unit.
+template <int THREADS>
+__device__ __forceinline__ Plan make_plan(const Groups& gr, int capacity, int G, int row_tile, int* lds, int* waves) {
+  Plan p;
+  p.own = lds;
+  p.reach = p.own + gr.R + 1;
+  p.group = p.reach + gr.R;
+  p.shared = p.group + gr.R;
+  p.least = p.shared + gr.n + 1;
+  int* least = p.least;
+  for (int g = threadIdx.x; g < gr.n; g += THREADS) least[g] = clamp_len(gr.prefix[g], capacity);
+  __syncthreads();
+  for (int r = threadIdx.x; r < gr.R; r += THREADS) {
+    int group = -1;
+    if (gr.n > 0) {
+      // the last group that starts at or before r
+      int lo = 0, hi = gr.n;  // starts[lo] <= r is not known for lo = 0
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (gr.start[mid] <= r) lo = mid;
+        else hi = mid;
+      }
+      const int s = max(gr.start[lo], 0), e = min(gr.start[lo + 1], gr.R);
+      if (s <= r && r < e && e - s > 1) {
+        // an empty member reads nothing and does not shorten what the others share
+        const int n = clamp_len(gr.lens[r], capacity);
+        if (n > 0) {
+          group = lo;
+          atomicMin(&least[lo], n);
+        }
+      }
+    }
+    p.group[r] = group;
+  }
+  __syncthreads();
+  for (int r = threadIdx.x; r < gr.R; r += THREADS) p.reach[r] = p.group[r] < 0 ? 0 : least[p.group[r]];
+  __syncthreads();
+  sums<THREADS>(gr.R, p.own, waves, [&](int r) {
+    const int n = clamp_len(gr.lens[r], capacity);
+    return tiles_of(own_from(n, p.reach[r], gr.window), n);
+  });
+  if (gr.n > 0)
+    sums<THREADS>(gr.n, p.shared, waves, [&](int g) {
+      const int s = max(gr.start[g], 0), e = min(gr.start[g + 1], gr.R);
+      return e - s > 1 ? ((e - s) * G + row_tile - 1) / row_tile * tiles_of(0, least[g]) : 0;
+    });
+  else if (threadIdx.x == 0)
+    p.shared[0] = 0;
+  __syncthreads();
+  return p;
+}
+
+// The last i of [0, n) with at[i] <= v; at[0] <= v.
+__device__ __forceinline__ int last_at(const int* at, int n, int v) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (at[mid] <= v) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// A line of `units` dealt to `wgs` workgroups: w has [first(w), first(w + 1)).
+struct Deal {
+  int64_t units;
+  int wgs;
+  __device__ __forceinline__ int first(int w) const { return (int)(w * units / wgs); }
+  __device__ __forceinline__ int owner(int64_t u) const { return (int)(((u + 1) * wgs - 1) / units); }
+};
+
+}  // namespace eldr
