@@ -41,8 +41,9 @@
  * Token slot j of request r lies in page block_table[r, j / block_size] at
  * offset j % block_size.  A slot whose page is outside [0, num_blocks) is
  * absent: it is not read, and counts as masked.  lens[r] tokens are cached;
- * it is taken as clamped to [0, N], N = max_blocks * block_size.  What pages
- * hold past lens[r] is never used, whatever its bits are.
+ * it is taken as clamped to [0, N], N = max_blocks * block_size, and as 0 where
+ * num_blocks is 0.  What pages hold past lens[r] is never used, whatever its
+ * bits are.
  *
  * Groups that share a prefix
  * --------------------------

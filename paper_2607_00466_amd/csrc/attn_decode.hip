@@ -19,15 +19,13 @@
 // meet in LDS at its end.  A segment that is a request's whole context gives
 // the output; the others leave sums that attn_join adds up.
 #include "attn_plan.hpp"
+#include "attn_tile.hpp"
 
 namespace eldr {
 
 constexpr int kDecodeThreads = 256;
 constexpr int kDecodeWaves = kDecodeThreads / kWave;
-constexpr int kRows = 16;       // query rows of a tile
-constexpr int kStep = 32;       // slots a wave takes at a time
 constexpr int kDecodeWgs = 768; // workgroups: three for each CU
-constexpr float kLog2e = 1.4426950408889634f;
 
 struct DecodeArgs {
   const uint16_t* q;
@@ -55,46 +53,6 @@ struct Parts {
 };
 
 static size_t parts_bytes(int64_t rows, int D) { return (2 * rows + (int64_t)kDecodeWgs * kRows) * (D + 4) * sizeof(float); }
-
-template <int D, bool FP8>
-struct Tile {
-  static constexpr int kK = D / 32;       // MFMA steps of the first product
-  static constexpr int kV = D / 16;       // value columns a lane holds
-  static constexpr int kElem = FP8 ? 1 : 2;
-
-  // Value index of the first of the 8 that a lane holds for step s.
-  static __device__ __forceinline__ int q_at(int s, int g) {
-    return FP8 ? (s / 2) * 64 + g * 16 + (s % 2) * 8 : s * 32 + g * 8;
-  }
-};
-
-// Two fp8 codes (bytes 0, 1 or 2, 3 of w) as bf16: exact.
-template <bool HI>
-__device__ __forceinline__ uint32_t fp8_pair(uint32_t w) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
-}
-
-// One 16-slot tile of keys as MFMA operands.
-template <int D, bool FP8>
-struct Keys {
-  using T = Tile<D, FP8>;
-  static constexpr int kLoads = FP8 ? T::kK / 2 : T::kK;
-  u32x4 raw[kLoads];
-  __device__ __forceinline__ void load(const char* rows, int n, int g) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-      raw[i] = *reinterpret_cast<const u32x4*>(rows + (uint32_t)(n * D * T::kElem + i * 64 + g * 16));
-  }
-  __device__ __forceinline__ u32x4 operand(int s) const {
-    if constexpr (FP8) {
-      const u32x4 r = raw[s / 2];
-      const uint32_t a = r[(s % 2) * 2], b = r[(s % 2) * 2 + 1];
-      return u32x4{fp8_pair<false>(a), fp8_pair<true>(a), fp8_pair<false>(b), fp8_pair<true>(b)};
-    } else {
-      return raw[s];
-    }
-  }
-};
 
 // 32 slots of values: the lane's kV columns of its 8 slots, 4 of each 16-slot
 // tile (rows 4 g .. 4 g + 3).
@@ -146,8 +104,6 @@ struct Values {
     return v;
   }
 };
-
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // A run of slots [k0, k1) of a request's (or group's) context against up to
 // kRows query rows.
@@ -491,7 +447,7 @@ extern "C" int moe_attn_decode(const uint16_t* q, const void* k_cache, const voi
   a.out = out, a.lse = lse, a.ws = static_cast<float*>(ws), a.scale = scale;
   a.Hq = d.Hq, a.G = d.Hq / d.Hkv, a.head_tiles = (a.G + eldr::kRows - 1) / eldr::kRows;
   eldr::Pages pg = pages_of(d, block_table);
-  if (d.num_blocks == 0) pg.max_blocks = 0;  // every slot is absent
+  if (d.num_blocks == 0) pg.max_blocks = 0;  // nothing is cached
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const bool fp8 = d.kv_type == MOE_KV_FP8;
   if (d.D == 64) return fp8 ? eldr::launch_decode<64, true>(a, pg, s) : eldr::launch_decode<64, false>(a, pg, s);

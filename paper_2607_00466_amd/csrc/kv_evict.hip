@@ -253,7 +253,7 @@ extern "C" int moe_kv_evict(const float* weights, const int32_t* pos, const int3
   eldr::EvictArgs a;
   a.weights = weights, a.pos = pos, a.lens = lens, a.seen = seen, a.protect = protect;
   a.src = src, a.new_lens = new_lens, a.weights_out = weights_out, a.pos_out = pos_out;
-  a.N = d.max_blocks * d.block_size, a.budget = budget, a.recent = recent;
+  a.N = d.num_blocks == 0 ? 0 : d.max_blocks * d.block_size, a.budget = budget, a.recent = recent;
   a.words = (a.N + 63) / 64;
   const size_t lds = (size_t)a.words * 12;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
@@ -265,7 +265,7 @@ extern "C" int moe_kv_evict(const float* weights, const int32_t* pos, const int3
   }
   hipLaunchKernelGGL(eldr::kv_select_kernel, dim3(d.R * d.Hkv), dim3(eldr::kSelectThreads), lds, s, a, d.Hkv);
   st = launch_status();
-  if (st != MOE_OK || a.N <= budget || d.num_blocks == 0) return st;
+  if (st != MOE_OK || a.N <= budget) return st;
   const int elem = d.kv_type == MOE_KV_FP8 ? 1 : 2;
   const int row_shift = __builtin_ctz((unsigned)(d.D * elem / 16));
   const dim3 grid((budget + eldr::kMoveSlots - 1) / eldr::kMoveSlots, d.R * d.Hkv);
