@@ -19,6 +19,7 @@
 // meet in LDS at its end.  A segment that is a request's whole context gives
 // the output; the others leave sums that attn_join adds up.
 #include "attn_plan.hpp"
+#include "attn_shared.hpp"
 #include "attn_tile.hpp"
 
 namespace eldr {
@@ -39,69 +40,20 @@ struct DecodeArgs {
   int32_t Hq, G, head_tiles;  // head_tiles: ceil(G / kRows)
 };
 
-// Where partial sums go: [rows][D] of sums and [rows][2] of (maximum, sum).
-// own, shared: rows of the requests' query heads (the segment that begins a
-// part); rest: kRows rows a workgroup (the one that continues a part).
+// The workspace: parts of rows, D sums then (maximum, sum) at a pitch of D + 4.
+// own, shared: by row of the requests' query heads, the part that begins a
+// request's own slots or its group's.  own_rest, shared_rest: by workgroup, the
+// part that continues one (the first stretch of a workgroup at most).  Then the
+// plan, for attn_join.
 struct Parts {
-  float *own, *shared, *rest;
-  int D;
-  __device__ Parts(float* ws, int64_t rows, int D) : D(D) {
+  float *own, *shared, *own_rest, *shared_rest;
+  int* plan;
+  __host__ __device__ Parts(float* ws, int64_t rows, int D, int shared_rows) {
     own = ws;
     shared = own + rows * (D + 4);
-    rest = shared + rows * (D + 4);
-  }
-};
-
-static size_t parts_bytes(int64_t rows, int D) { return (2 * rows + (int64_t)kDecodeWgs * kRows) * (D + 4) * sizeof(float); }
-
-// 32 slots of values: the lane's kV columns of its 8 slots, 4 of each 16-slot
-// tile (rows 4 g .. 4 g + 3).
-template <int D, bool FP8>
-struct Values {
-  using T = Tile<D, FP8>;
-  static constexpr int kBytes = T::kV * T::kElem;  // a slot's, 4 to 32
-  static constexpr int kWords = kBytes / 4;
-  uint32_t raw[8][kWords];
-  __device__ __forceinline__ void load(const char* lo, const char* hi, int n, int g) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const char* p = (j < 4 ? lo : hi) + (uint32_t)((4 * g + (j & 3)) * D * T::kElem + n * kBytes);
-      if constexpr (kBytes >= 16) {
-#pragma unroll
-        for (int w = 0; w < kWords; w += 4) {
-          const u32x4 x = *reinterpret_cast<const u32x4*>(p + 4 * w);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) raw[j][w + i] = x[i];
-        }
-      } else if constexpr (kBytes == 8) {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(p);
-        raw[j][0] = x[0], raw[j][1] = x[1];
-      } else {
-        raw[j][0] = *reinterpret_cast<const uint32_t*>(p);
-      }
-    }
-  }
-  // Slots that do not count must not reach a product: 0 times their bits may be NaN.
-  __device__ __forceinline__ void drop(int j, bool keep) {
-#pragma unroll
-    for (int w = 0; w < kWords; ++w) raw[j][w] = keep ? raw[j][w] : 0u;
-  }
-  // Column c of the lane's 8 slots.
-  __device__ __forceinline__ u32x4 operand(int c) const {
-    u32x4 v;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t *a = raw[2 * i], *b = raw[2 * i + 1];
-      if constexpr (FP8) {
-        // the pair's bytes side by side, then both to bf16
-        const uint32_t sel = (c & 2) ? 0x07030602u : 0x05010400u;
-        const uint32_t z = __builtin_amdgcn_perm(b[c / 4], a[c / 4], sel);
-        v[i] = (c & 1) ? fp8_pair<true>(z) : fp8_pair<false>(z);
-      } else {
-        v[i] = __builtin_amdgcn_perm(b[c / 2], a[c / 2], (c & 1) ? 0x07060302u : 0x05040100u);
-      }
-    }
-    return v;
+    own_rest = shared + rows * (D + 4);
+    shared_rest = own_rest + (int64_t)kDecodeWgs * kRows * (D + 4);
+    plan = reinterpret_cast<int*>(shared_rest + (int64_t)kSharedWgs * shared_rows * (D + 4));
   }
 };
 
@@ -261,75 +213,39 @@ __device__ __forceinline__ void merge(const DecodeArgs& a, const Segment& sg, fl
 }
 
 template <int D, bool FP8>
-__global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void attn_decode_kernel(DecodeArgs a, Pages pg, int64_t rows) {
+__global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void attn_decode_kernel(DecodeArgs a, Pages pg, Parts parts) {
   extern __shared__ int lds[];
   __shared__ int waves[kDecodeWaves];
   float* sums_lds = reinterpret_cast<float*>(lds);
   int* plan_lds = lds + kDecodeWaves * kRows * (D + 4);
   const int capacity = pg.capacity();
-  const Plan plan = make_plan<kDecodeThreads>(a.gr, capacity, a.G, kRows, plan_lds, waves);
-  const Parts parts(a.ws, rows, D);
-  const int R = a.gr.R, n = a.gr.n, wgs = gridDim.x;
-  const int heads = pg.Hkv * a.head_tiles;
-  const int own_row = plan.own[R], shared_row = plan.shared[n];
-  const int64_t own_units = (int64_t)own_row * heads, shared_units = (int64_t)shared_row * pg.Hkv;
-  // workgroups for each line, by its share of the units; none without a unit (the join counts on it)
-  int shared_wgs = 0;
-  if (shared_units > 0) {
-    shared_wgs = own_units == 0 ? wgs : min(max((int)(wgs * shared_units / (own_units + shared_units)), 1), wgs - 1);
-    shared_wgs = (int)min((int64_t)shared_wgs, shared_units);
-  }
-  const int own_wgs = (int)min((int64_t)(wgs - shared_wgs), own_units);
-  float* after = parts.rest + (int64_t)wgs * kRows * (D + 4);
+  const Plan plan = make_plan<kDecodeThreads>(a.gr, capacity, a.G, SharedTile<D>::kRowsWg, plan_lds, waves);
+  const int R = a.gr.R, n = a.gr.n, row = plan.own[R];
   if (blockIdx.x == 0) {
-    // for attn_join: the deal and the plan
-    int* to = reinterpret_cast<int*>(after);
-    if (threadIdx.x == 0) to[0] = own_wgs, to[1] = shared_wgs;
-    const int ints = 3 * R + 1 + n + 1;
-    for (int i = threadIdx.x; i < ints; i += kDecodeThreads) to[4 + i] = plan.own[i];
+    const int ints = 3 * R + 1 + n + 1;  // own, reach, group, shared
+    for (int i = threadIdx.x; i < ints; i += kDecodeThreads) parts.plan[i] = plan.own[i];
   }
-  if ((int)blockIdx.x >= shared_wgs + own_wgs) return;
-  const bool is_shared = (int)blockIdx.x < shared_wgs;
-  const int w = is_shared ? blockIdx.x : blockIdx.x - shared_wgs;
-  const Deal deal = is_shared ? Deal{shared_units, shared_wgs} : Deal{own_units, own_wgs};
-  int u = __builtin_amdgcn_readfirstlane(deal.first(w));
-  const int end = __builtin_amdgcn_readfirstlane(deal.first(w + 1));
-  float* rest = parts.rest + (int64_t)blockIdx.x * kRows * (D + 4);
+  const Deal deal = deal_of((int64_t)row * pg.Hkv * a.head_tiles, kDecodeWgs);
+  if ((int)blockIdx.x >= deal.wgs) return;
+  int u = __builtin_amdgcn_readfirstlane(deal.first(blockIdx.x));
+  const int end = __builtin_amdgcn_readfirstlane(deal.first(blockIdx.x + 1));
   float m, l;
   f32x4 acc[D / 16];
   while (u < end) {
-    Segment sg;
-    bool whole = false, begins;
-    int tiles;
-    if (is_shared) {
-      const int h = u / shared_row, v = u - h * shared_row;
-      const int grp = last_at(plan.shared, n, v);
-      const int first = max(a.gr.start[grp], 0), members = min(a.gr.start[grp + 1], R) - first;
-      const int reach = plan.least[grp];
-      const int per = tiles_of(0, reach), in = v - plan.shared[grp];
-      const int tile = in / per, t = in - tile * per;
-      tiles = min(per - t, end - u);
-      begins = t == 0;
-      sg.table_row = first, sg.first = first, sg.rows = members * a.G, sg.row0 = tile * kRows, sg.h = h;
-      sg.k0 = t * kTile, sg.k1 = min((t + tiles) * kTile, reach);
-    } else {
-      const int hv = u / own_row, v = u - hv * own_row;
-      const int r = last_at(plan.own, R, v), t = v - plan.own[r];
-      const int len = clamp_len(a.gr.lens[r], capacity), reach = plan.reach[r];
-      const int lo = own_from(len, reach, a.gr.window), t0 = lo / kTile;
-      tiles = min(plan.own[r + 1] - v, end - u);
-      begins = t == 0;
-      whole = begins && v + tiles == plan.own[r + 1] && reach == 0;
-      sg.table_row = r, sg.first = r, sg.rows = a.G, sg.row0 = hv % a.head_tiles * kRows, sg.h = hv / a.head_tiles;
-      sg.k0 = max((t0 + t) * kTile, lo), sg.k1 = min((t0 + t + tiles) * kTile, len);
-    }
+    const int hv = u / row, v = u - hv * row;
+    const int r = last_at(plan.own, R, v), t = v - plan.own[r];
+    const int len = clamp_len(a.gr.lens[r], capacity), reach = plan.reach[r];
+    const int lo = own_from(len, reach, a.gr.window), t0 = lo / kTile;
+    const int tiles = __builtin_amdgcn_readfirstlane(min(plan.own[r + 1] - v, end - u));
+    const bool begins = t == 0, whole = begins && v + tiles == plan.own[r + 1] && reach == 0;
+    Segment sg{r, r, a.G, hv % a.head_tiles * kRows, hv / a.head_tiles, max((t0 + t) * kTile, lo), min((t0 + t + tiles) * kTile, len)};
     // the same for every lane: keep it in scalar registers
     int* f = reinterpret_cast<int*>(&sg);
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(sg) / 4); ++i) f[i] = __builtin_amdgcn_readfirstlane(f[i]);
-    tiles = __builtin_amdgcn_readfirstlane(tiles);
     attend<D, FP8>(a, pg, sg, m, l, acc);
-    merge<D, FP8>(a, sg, m, l, acc, sums_lds, whole, begins ? (is_shared ? parts.shared : parts.own) : rest, begins);
+    merge<D, FP8>(a, sg, m, l, acc, sums_lds, whole,
+                  begins ? parts.own : parts.own_rest + (int64_t)blockIdx.x * kRows * (D + 4), begins);
     u += tiles;
   }
 }
@@ -337,18 +253,15 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void attn_decode_
 // Adds up the parts of the rows that have several, and writes the rows that
 // have none: a wave a (request, query head).
 template <int D, bool FP8>
-__global__ __launch_bounds__(kDecodeThreads) void attn_join_kernel(DecodeArgs a, Pages pg, int64_t rows, int wgs) {
+__global__ __launch_bounds__(kDecodeThreads) void attn_join_kernel(DecodeArgs a, Pages pg, Parts parts, int64_t rows) {
   constexpr int kPer = D / kWave;
   const int lane = threadIdx.x % kWave;
   const int64_t q_row = (int64_t)blockIdx.x * kDecodeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   if (q_row >= rows) return;
-  const Parts parts(a.ws, rows, D);
-  const int* head = reinterpret_cast<const int*>(parts.rest + (int64_t)wgs * kRows * (D + 4));
   const int R = a.gr.R, n = a.gr.n;
-  const int* own = head + 4;
+  const int* own = parts.plan;
   const int *reach = own + R + 1, *group = reach + R, *shared = group + R;
   const int r = (int)(q_row / a.Hq), hq = (int)(q_row % a.Hq), h = hq / a.G, i = hq % a.G;
-  const int own_wgs = head[0], shared_wgs = head[1];
   const int own_row = own[R], tiles = own[r + 1] - own[r], mine = reach[r];
   const int64_t stride = D + 4;
   float top = -INFINITY, sum = 0.0f, o[kPer] = {};
@@ -364,23 +277,23 @@ __global__ __launch_bounds__(kDecodeThreads) void attn_join_kernel(DecodeArgs a,
   int parts_here = 0;
   if (mine > 0) {
     const int g = group[r];
-    const int row = (r - max(a.gr.start[g], 0)) * a.G + i, tile = row / kRows;
-    const int per = tiles_of(0, mine);
-    const int64_t u0 = (int64_t)h * shared[n] + shared[g] + (int64_t)tile * per;
-    const Deal deal{(int64_t)shared[n] * pg.Hkv, shared_wgs};
+    constexpr int kTileRows = SharedTile<D>::kRowsWg;
+    const int row = (r - max(a.gr.start[g], 0)) * a.G + i, per = tiles_of(0, mine);
+    const int64_t u0 = (int64_t)h * shared[n] + shared[g] + (int64_t)(row / kTileRows) * per;
+    const Deal deal = deal_of((int64_t)shared[n] * pg.Hkv, kSharedWgs);
     const int w0 = deal.owner(u0), w1 = deal.owner(u0 + per - 1);
     add(parts.shared + q_row * stride);
-    for (int w = w0 + 1; w <= w1; ++w) add(parts.rest + ((int64_t)w * kRows + row % kRows) * stride);
+    for (int w = w0 + 1; w <= w1; ++w) add(parts.shared_rest + ((int64_t)w * kTileRows + row % kTileRows) * stride);
     parts_here += 2;
   }
   if (tiles > 0) {
-    const Deal deal{(int64_t)own_row * pg.Hkv * a.head_tiles, own_wgs};
+    const Deal deal = deal_of((int64_t)own_row * pg.Hkv * a.head_tiles, kDecodeWgs);
     const int64_t u0 = (int64_t)(h * a.head_tiles + i / kRows) * own_row + own[r];
     const int w0 = deal.owner(u0), w1 = deal.owner(u0 + tiles - 1);
     parts_here += 1 + w1 - w0;
     if (parts_here == 1) return;  // written already
     add(parts.own + q_row * stride);
-    for (int w = w0 + 1; w <= w1; ++w) add(parts.rest + ((int64_t)(shared_wgs + w) * kRows + i % kRows) * stride);
+    for (int w = w0 + 1; w <= w1; ++w) add(parts.own_rest + ((int64_t)w * kRows + i % kRows) * stride);
   }
   if (a.sinks) {
     const float sink = a.sinks[hq] * kLog2e, with = fmaxf(top, sink), f = exp2_fast(top - with);
@@ -396,29 +309,48 @@ __global__ __launch_bounds__(kDecodeThreads) void attn_join_kernel(DecodeArgs a,
     a.lse[q_row] = sum > 0.0f ? (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
 }
 
+// Raises a kernel's dynamic LDS limit where a launch needs more than the default.
+inline bool lds_allowed(const void* kernel, size_t bytes) {
+  if (bytes <= 60 * 1024) return true;
+  if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess) return true;
+  (void)hipGetLastError();
+  return false;
+}
+
 template <int D, bool FP8>
 int launch_decode(const DecodeArgs& a, const Pages& pg, hipStream_t s) {
+  using S = SharedTile<D>;
   const int64_t rows = (int64_t)a.gr.R * a.Hq;
-  const size_t lds = (size_t)kDecodeWaves * kRows * (D + 4) * 4 + Plan::bytes(a.gr.R, a.gr.n);
-  if (lds > 64 * 1024 - 256) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void*>(attn_decode_kernel<D, FP8>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
-      (void)hipGetLastError();
-      return MOE_ERR_HIP;
-    }
+  const Parts parts(a.ws, rows, D, S::kRowsWg);
+  const size_t plan = Plan::bytes(a.gr.R, a.gr.n);
+  const size_t lds = (size_t)kDecodeWaves * kRows * (D + 4) * 4 + plan;
+  if (!lds_allowed(reinterpret_cast<const void*>(attn_decode_kernel<D, FP8>), lds)) return MOE_ERR_HIP;
+  if (a.gr.n > 0) {
+    const SharedArgs sh{a.q, a.k_cache, a.v_cache, a.gr, a.k_scale, parts.shared, parts.shared_rest, a.scale, a.Hq, a.G};
+    if (!lds_allowed(reinterpret_cast<const void*>(attn_shared_kernel<D, FP8>), S::kBytes + plan)) return MOE_ERR_HIP;
+    hipLaunchKernelGGL((attn_shared_kernel<D, FP8>), dim3(kSharedWgs), dim3(kSharedThreads), S::kBytes + plan, s, sh, pg);
   }
-  hipLaunchKernelGGL((attn_decode_kernel<D, FP8>), dim3(kDecodeWgs), dim3(kDecodeThreads), lds, s, a, pg, rows);
+  hipLaunchKernelGGL((attn_decode_kernel<D, FP8>), dim3(kDecodeWgs), dim3(kDecodeThreads), lds, s, a, pg, parts);
   hipLaunchKernelGGL((attn_join_kernel<D, FP8>), dim3((unsigned)((rows + kDecodeWaves - 1) / kDecodeWaves)),
-                     dim3(kDecodeThreads), 0, s, a, pg, rows, kDecodeWgs);
+                     dim3(kDecodeThreads), 0, s, a, pg, parts, rows);
   return eldr_host::launch_status();
+}
+
+template <int D>
+size_t decode_workspace(int64_t rows, int R) {
+  const Parts p(nullptr, rows, D, SharedTile<D>::kRowsWg);
+  // the plan of at most MOE_ATTN_MAX_R groups
+  return reinterpret_cast<uintptr_t>(p.plan) + Plan::bytes(R, MOE_ATTN_MAX_R);
 }
 
 }  // namespace eldr
 
 extern "C" size_t moe_attn_workspace_bytes(moe_attn_dims d) {
   if (eldr_host::check_attn_dims(d) != MOE_OK) return 0;
-  // the parts, then the plan of at most R groups
-  return eldr::parts_bytes((int64_t)d.R * d.Hq, d.D) + 16 + eldr::Plan::bytes(d.R, MOE_ATTN_MAX_R);
+  const int64_t rows = (int64_t)d.R * d.Hq;
+  return d.D == 64    ? eldr::decode_workspace<64>(rows, d.R)
+         : d.D == 128 ? eldr::decode_workspace<128>(rows, d.R)
+                      : eldr::decode_workspace<256>(rows, d.R);
 }
 
 extern "C" int moe_attn_decode(const uint16_t* q, const void* k_cache, const void* v_cache,

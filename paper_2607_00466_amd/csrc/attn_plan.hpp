@@ -9,6 +9,8 @@
 //
 //   own line     for each head tile, for each request: tiles of kTile slots
 //   shared line  for each kv head, for each group, for each row tile: tiles
+//
+// A part of a row is a stretch that one workgroup holds.
 #pragma once
 
 #include "attn_common.hpp"
@@ -147,5 +149,8 @@ struct Deal {
   __device__ __forceinline__ int first(int w) const { return (int)(w * units / wgs); }
   __device__ __forceinline__ int owner(int64_t u) const { return (int)(((u + 1) * wgs - 1) / units); }
 };
+
+// No workgroup without a unit: the join counts on it.
+__device__ __forceinline__ Deal deal_of(int64_t units, int wgs) { return Deal{units, (int)min((int64_t)wgs, units)}; }
 
 }  // namespace eldr

@@ -52,4 +52,55 @@ struct Keys {
   }
 };
 
+// 32 slots of values: the lane's kV columns of its 8 slots, 4 of each 16-slot
+// tile (rows 4 g .. 4 g + 3).
+template <int D, bool FP8>
+struct Values {
+  using T = Tile<D, FP8>;
+  static constexpr int kBytes = T::kV * T::kElem;  // a slot's, 4 to 32
+  static constexpr int kWords = kBytes / 4;
+  uint32_t raw[8][kWords];
+  __device__ __forceinline__ void load(const char* lo, const char* hi, int n, int g) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const char* p = (j < 4 ? lo : hi) + (uint32_t)((4 * g + (j & 3)) * D * T::kElem + n * kBytes);
+      if constexpr (kBytes >= 16) {
+#pragma unroll
+        for (int w = 0; w < kWords; w += 4) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(p + 4 * w);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) raw[j][w + i] = x[i];
+        }
+      } else if constexpr (kBytes == 8) {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+        raw[j][0] = x[0], raw[j][1] = x[1];
+      } else {
+        raw[j][0] = *reinterpret_cast<const uint32_t*>(p);
+      }
+    }
+  }
+  // Slots that do not count must not reach a product: 0 times their bits may be NaN.
+  __device__ __forceinline__ void drop(int j, bool keep) {
+#pragma unroll
+    for (int w = 0; w < kWords; ++w) raw[j][w] = keep ? raw[j][w] : 0u;
+  }
+  // Column c of the lane's 8 slots.
+  __device__ __forceinline__ u32x4 operand(int c) const {
+    u32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t *a = raw[2 * i], *b = raw[2 * i + 1];
+      if constexpr (FP8) {
+        // the pair's bytes side by side, then both to bf16
+        const uint32_t sel = (c & 2) ? 0x07030602u : 0x05010400u;
+        const uint32_t z = __builtin_amdgcn_perm(b[c / 4], a[c / 4], sel);
+        v[i] = (c & 1) ? fp8_pair<true>(z) : fp8_pair<false>(z);
+      } else {
+        v[i] = __builtin_amdgcn_perm(b[c / 2], a[c / 2], (c & 1) ? 0x07060302u : 0x05040100u);
+      }
+    }
+    return v;
+  }
+};
+
 }  // namespace eldr
