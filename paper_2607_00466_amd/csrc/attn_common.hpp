@@ -9,6 +9,15 @@ namespace eldr {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
+// A load through the scalar cache: p is the same for the whole wave, and nothing
+// writes there while the kernel runs.  (Without the constant address space the
+// compiler has to use a vector load, whose wait also waits for every tile that
+// was asked for before it.)
+template <typename T>
+__device__ __forceinline__ T uniform_load(const T* p) {
+  return *reinterpret_cast<const __attribute__((address_space(4))) T*>(reinterpret_cast<uintptr_t>(p));
+}
+
 // The kernels' view of one cache: pages of block_size = 1 << shift slots.
 struct Pages {
   const int32_t* table;  // [R, max_blocks]

@@ -87,16 +87,17 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, const Pages& pg, con
 #pragma unroll
     for (int s = 0; s < T::kK; ++s) {
       const u32x4 x = *reinterpret_cast<const u32x4*>(src + T::q_at(s, g));
-      q[s] = live ? x : u32x4{0u, 0u, 0u, 0u};
+      q[s] = keep_if(live, x);
     }
   }
   const float unit = a.scale * kLog2e * (FP8 && a.k_scale ? a.k_scale[sg.h] : 1.0f);
   const int32_t* table = pg.table + (int64_t)sg.table_row * pg.max_blocks;
-  for (int k = sg.k0 / kStep * kStep + wave * kStep; k < sg.k1; k += kDecodeWaves * kStep) {
-    // the step's two 16-slot tiles, each inside a page
-    const int b0 = table[k >> pg.shift];
-    const int next = (k + 16) >> pg.shift;
-    const int b1 = next < pg.max_blocks ? table[next] : -1;
+  const int k_first = sg.k0 / kStep * kStep + wave * kStep;
+  // a step's pages are looked up one step ahead
+  StepPages pages = step_pages(pg, table, k_first);
+  for (int k = k_first; k < sg.k1; k += kDecodeWaves * kStep) {
+    const int b0 = pages.b0, b1 = pages.b1;
+    pages = step_pages(pg, table, k + kDecodeWaves * kStep);
     const bool has0 = pg.has(b0), has1 = pg.has(b1);
     const bool whole = has0 && has1 && k >= sg.k0 && k + kStep <= sg.k1;
     const int64_t r0 = pg.row(has0 ? b0 : 0, sg.h, k) * T::kElem, r1 = pg.row(has1 ? b1 : 0, sg.h, k + 16) * T::kElem;
@@ -112,39 +113,18 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, const Pages& pg, con
       s[0] = mfma16x16x32(k_lo.operand(i), q[i], s[0]);
       s[1] = mfma16x16x32(k_hi.operand(i), q[i], s[1]);
     }
-    float x[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = s[j / 4][j % 4] * unit;
+    const auto keep = [&](int j) {
+      const int at = k + (j / 4) * 16 + 4 * g + j % 4;
+      return (j < 4 ? has0 : has1) && at >= sg.k0 && at < sg.k1;
+    };
     if (!whole) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int at = k + (j / 4) * 16 + 4 * g + j % 4;
-        const bool keep = (j < 4 ? has0 : has1) && at >= sg.k0 && at < sg.k1;
-        x[j] = keep ? x[j] : -INFINITY;
-        v.drop(j, keep);
-      }
+      for (int j = 0; j < 8; ++j) v.drop(j, keep(j));
     }
-    float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    if (__any(top > m)) {
-      const float m2 = fmaxf(m, top);
-      const float back = exp2_fast(m - (m2 == -INFINITY ? 0.0f : m2));
-      m = m2;
-      l *= back;
+    const u32x4 p = softmax_step(s, unit, whole, keep, m, l, [&](float f) {
 #pragma unroll
-      for (int c = 0; c < T::kV; ++c) acc[c] *= back;
-    }
-    const float base = m == -INFINITY ? 0.0f : m;
-    u32x4 p;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      x[j] = exp2_fast(x[j] - base);
-      l += x[j];
-    }
-    // rounded to bf16 for the product alone: the sum keeps the weights' 32 bits
-#pragma unroll
-    for (int i = 0; i < 4; ++i) p[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+      for (int c = 0; c < T::kV; ++c) acc[c] *= f;
+    });
 #pragma unroll
     for (int c = 0; c < T::kV; ++c) acc[c] = mfma16x16x32(v.operand(c), p, acc[c]);
   }
@@ -206,7 +186,7 @@ __device__ __forceinline__ void merge(const DecodeArgs& a, const Segment& sg, fl
     } else {
       float* to = part + (by_row ? q_row : (int64_t)row) * (D + 4);
       *reinterpret_cast<f32x4*>(to + at) = o;
-      if (at == 0) to[D] = top, to[D + 1] = sum;
+      if (at == 0) *reinterpret_cast<f32x4*>(to + D) = f32x4{top, sum, 0.0f, 0.0f};
     }
   }
   __syncthreads();
@@ -225,7 +205,7 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void attn_decode_
     const int ints = 3 * R + 1 + n + 1;  // own, reach, group, shared
     for (int i = threadIdx.x; i < ints; i += kDecodeThreads) parts.plan[i] = plan.own[i];
   }
-  const Deal deal = deal_of((int64_t)row * pg.Hkv * a.head_tiles, kDecodeWgs);
+  const Deal deal(row * pg.Hkv * a.head_tiles, kDecodeWgs);
   if ((int)blockIdx.x >= deal.wgs) return;
   int u = __builtin_amdgcn_readfirstlane(deal.first(blockIdx.x));
   const int end = __builtin_amdgcn_readfirstlane(deal.first(blockIdx.x + 1));
@@ -250,63 +230,100 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void attn_decode_
   }
 }
 
-// Adds up the parts of the rows that have several, and writes the rows that
-// have none: a wave a (request, query head).
-template <int D, bool FP8>
-__global__ __launch_bounds__(kDecodeThreads) void attn_join_kernel(DecodeArgs a, Pages pg, Parts parts, int64_t rows) {
-  constexpr int kPer = D / kWave;
-  const int lane = threadIdx.x % kWave;
-  const int64_t q_row = (int64_t)blockIdx.x * kDecodeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  if (q_row >= rows) return;
+// Adds up the parts of a row that has several, and writes a row that has none.
+// THREADS threads (64, or 256 where there are few rows, each of them in many
+// parts) take a (request, query head): sets of D / 4 of them take a part, four
+// values each, and take the parts in turn, with a running maximum; the sets meet
+// in LDS.
+template <int D, bool FP8, int THREADS>
+__global__ __launch_bounds__(kDecodeThreads) void attn_join_kernel(DecodeArgs a, Pages pg, Parts parts, int rows) {
+  constexpr int kSet = D / 4, kSets = THREADS / kSet, kRowsWg = kDecodeThreads / THREADS;
+  constexpr int kPitch = D + 4;
+  __shared__ f32x4 sums_of[kRowsWg][kSets][kSet];
+  __shared__ float tops_of[kRowsWg][kSets], totals_of[kRowsWg][kSets];
+  const int mine_row = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
+  const bool real = (int)blockIdx.x * kRowsWg + mine_row < rows;
+  const int q_row = real ? blockIdx.x * kRowsWg + mine_row : 0;
+  auto& sums = sums_of[mine_row];
+  auto &tops = tops_of[mine_row], &totals = totals_of[mine_row];
   const int R = a.gr.R, n = a.gr.n;
   const int* own = parts.plan;
   const int *reach = own + R + 1, *group = reach + R, *shared = group + R;
-  const int r = (int)(q_row / a.Hq), hq = (int)(q_row % a.Hq), h = hq / a.G, i = hq % a.G;
+  const int r = q_row / a.Hq, hq = q_row - r * a.Hq, h = hq / a.G, i = hq - h * a.G;
   const int own_row = own[R], tiles = own[r + 1] - own[r], mine = reach[r];
-  const int64_t stride = D + 4;
-  float top = -INFINITY, sum = 0.0f, o[kPer] = {};
-  const auto add = [&](const float* p) {
-    const float pm = p[D], ps = p[D + 1];
-    const float m2 = fmaxf(top, pm), base = m2 == -INFINITY ? 0.0f : m2;
-    const float f = exp2_fast(top - base), e = exp2_fast(pm - base);
-    sum = sum * f + ps * e;
-#pragma unroll
-    for (int c = 0; c < kPer; ++c) o[c] = o[c] * f + p[c * kWave + lane] * e;
-    top = m2;
-  };
-  int parts_here = 0;
+  // the row's parts: the first by row, the others by the workgroups after w0
+  int shared_parts = 0, shared_w0 = 0, shared_at = 0, own_parts = 0, own_w0 = 0;
+  constexpr int kTileRows = SharedTile<D>::kRowsWg;
   if (mine > 0) {
     const int g = group[r];
-    constexpr int kTileRows = SharedTile<D>::kRowsWg;
     const int row = (r - max(a.gr.start[g], 0)) * a.G + i, per = tiles_of(0, mine);
-    const int64_t u0 = (int64_t)h * shared[n] + shared[g] + (int64_t)(row / kTileRows) * per;
-    const Deal deal = deal_of((int64_t)shared[n] * pg.Hkv, kSharedWgs);
-    const int w0 = deal.owner(u0), w1 = deal.owner(u0 + per - 1);
-    add(parts.shared + q_row * stride);
-    for (int w = w0 + 1; w <= w1; ++w) add(parts.shared_rest + ((int64_t)w * kTileRows + row % kTileRows) * stride);
-    parts_here += 2;
+    const int u0 = h * shared[n] + shared[g] + row / kTileRows * per;
+    const Deal deal(shared[n] * pg.Hkv, kSharedWgs);
+    shared_w0 = deal.owner(u0);
+    shared_parts = deal.owner(u0 + per - 1) - shared_w0 + 1;
+    shared_at = row % kTileRows;
   }
   if (tiles > 0) {
-    const Deal deal = deal_of((int64_t)own_row * pg.Hkv * a.head_tiles, kDecodeWgs);
-    const int64_t u0 = (int64_t)(h * a.head_tiles + i / kRows) * own_row + own[r];
-    const int w0 = deal.owner(u0), w1 = deal.owner(u0 + tiles - 1);
-    parts_here += 1 + w1 - w0;
-    if (parts_here == 1) return;  // written already
-    add(parts.own + q_row * stride);
-    for (int w = w0 + 1; w <= w1; ++w) add(parts.own_rest + ((int64_t)w * kRows + i % kRows) * stride);
+    const Deal deal(own_row * pg.Hkv * a.head_tiles, kDecodeWgs);
+    const int u0 = (h * a.head_tiles + i / kRows) * own_row + own[r];
+    own_w0 = deal.owner(u0);
+    own_parts = deal.owner(u0 + tiles - 1) - own_w0 + 1;
+  }
+  const bool written = !real || (own_parts == 1 && shared_parts == 0);  // by attn_decode
+  const int set = threadIdx.x % THREADS / kSet, at = threadIdx.x % kSet;
+  const int64_t first = (int64_t)q_row * kPitch;
+  const auto part = [&](int p) -> const float* {
+    if (p < shared_parts)
+      return p == 0 ? parts.shared + first : parts.shared_rest + ((int64_t)(shared_w0 + p) * kTileRows + shared_at) * kPitch;
+    p -= shared_parts;
+    return p == 0 ? parts.own + first : parts.own_rest + ((int64_t)(own_w0 + p) * kRows + i % kRows) * kPitch;
+  };
+  const int count = written ? 0 : shared_parts + own_parts;
+  constexpr int kBatch = 4;  // parts that a set has in flight
+  float top = -INFINITY, total = 0.0f;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = set; p0 < count; p0 += kBatch * kSets) {
+    f32x4 v[kBatch], ml[kBatch];
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      const float* from = part(min(p0 + b * kSets, count - 1));
+      v[b] = *reinterpret_cast<const f32x4*>(from + 4 * at);
+      ml[b] = *reinterpret_cast<const f32x4*>(from + D);
+    }
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      const bool there = p0 + b * kSets < count;
+      const float pm = there ? ml[b][0] : -INFINITY;
+      const float m2 = fmaxf(top, pm), base = m2 == -INFINITY ? 0.0f : m2;
+      const float f = exp2_fast(top - base), e = exp2_fast(pm - base);
+      total = total * f + ml[b][1] * e;
+      sum = sum * f + v[b] * e;
+      top = m2;
+    }
+  }
+  sums[set][at] = sum;
+  if (at == 0) tops[set] = top, totals[set] = total;
+  __syncthreads();
+  if (written || set != 0) return;
+#pragma unroll
+  for (int s = 1; s < kSets; ++s) {
+    const float m2 = fmaxf(top, tops[s]), base = m2 == -INFINITY ? 0.0f : m2;
+    const float f = exp2_fast(top - base), e = exp2_fast(tops[s] - base);
+    total = total * f + totals[s] * e;
+    sum = sum * f + sums[s][at] * e;
+    top = m2;
   }
   if (a.sinks) {
     const float sink = a.sinks[hq] * kLog2e, with = fmaxf(top, sink), f = exp2_fast(top - with);
-    sum = sum * f + exp2_fast(sink - with);
-#pragma unroll
-    for (int c = 0; c < kPer; ++c) o[c] *= f;
+    total = total * f + exp2_fast(sink - with);
+    sum *= f;
     top = with;
   }
-  const float by = sum > 0.0f ? (FP8 && a.v_scale ? a.v_scale[h] : 1.0f) / sum : 0.0f;
-#pragma unroll
-  for (int c = 0; c < kPer; ++c) a.out[q_row * D + c * kWave + lane] = (uint16_t)pack_bf16(o[c] * by, 0.0f);
-  if (lane == 0 && a.lse)
-    a.lse[q_row] = sum > 0.0f ? (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
+  const float by = total > 0.0f ? (FP8 && a.v_scale ? a.v_scale[h] : 1.0f) / total : 0.0f;
+  *reinterpret_cast<u32x2*>(a.out + (int64_t)q_row * D + 4 * at) =
+      u32x2{pack_bf16(sum[0] * by, sum[1] * by), pack_bf16(sum[2] * by, sum[3] * by)};
+  if (at == 0 && a.lse)
+    a.lse[q_row] = total > 0.0f ? (top + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
 }
 
 // Raises a kernel's dynamic LDS limit where a launch needs more than the default.
@@ -331,8 +348,14 @@ int launch_decode(const DecodeArgs& a, const Pages& pg, hipStream_t s) {
     hipLaunchKernelGGL((attn_shared_kernel<D, FP8>), dim3(kSharedWgs), dim3(kSharedThreads), S::kBytes + plan, s, sh, pg);
   }
   hipLaunchKernelGGL((attn_decode_kernel<D, FP8>), dim3(kDecodeWgs), dim3(kDecodeThreads), lds, s, a, pg, parts);
-  hipLaunchKernelGGL((attn_join_kernel<D, FP8>), dim3((unsigned)((rows + kDecodeWaves - 1) / kDecodeWaves)),
-                     dim3(kDecodeThreads), 0, s, a, pg, parts, rows);
+  // measured (us): 64 rows of 192 parts 8 by 256 threads and 31 by 64; 16,384 rows of
+  // about 10 parts 39 and 14
+  constexpr int64_t kFewRows = 1024;
+  if (rows <= kFewRows)
+    hipLaunchKernelGGL((attn_join_kernel<D, FP8, 256>), dim3((unsigned)rows), dim3(kDecodeThreads), 0, s, a, pg, parts, (int)rows);
+  else
+    hipLaunchKernelGGL((attn_join_kernel<D, FP8, 64>), dim3((unsigned)((rows + 3) / 4)), dim3(kDecodeThreads), 0, s, a, pg, parts,
+                       (int)rows);
   return eldr_host::launch_status();
 }
 

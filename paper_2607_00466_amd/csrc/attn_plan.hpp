@@ -142,15 +142,22 @@ __device__ __forceinline__ int last_at(const int* at, int n, int v) {
   return lo;
 }
 
-// A line of `units` dealt to `wgs` workgroups: w has [first(w), first(w + 1)).
+// A line of units dealt to workgroups in stretches whose lengths differ by one
+// at most: w has [first(w), first(w + 1)), the first `longer` ones each + 1 units.
+// No workgroup is without a unit: the join counts on it.
 struct Deal {
-  int64_t units;
-  int wgs;
-  __device__ __forceinline__ int first(int w) const { return (int)(w * units / wgs); }
-  __device__ __forceinline__ int owner(int64_t u) const { return (int)(((u + 1) * wgs - 1) / units); }
+  int wgs, each, longer;
+  __device__ __forceinline__ Deal(int units, int most) {
+    wgs = min(units, most);
+    each = wgs > 0 ? (int)((uint32_t)units / (uint32_t)wgs) : 1;
+    longer = units - each * wgs;
+  }
+  __device__ __forceinline__ int first(int w) const { return w * each + min(w, longer); }
+  __device__ __forceinline__ int owner(int u) const {
+    const int in_longer = longer * (each + 1);
+    return u < in_longer ? (int)((uint32_t)u / (uint32_t)(each + 1))
+                         : longer + (int)((uint32_t)(u - in_longer) / (uint32_t)each);
+  }
 };
-
-// No workgroup without a unit: the join counts on it.
-__device__ __forceinline__ Deal deal_of(int64_t units, int wgs) { return Deal{units, (int)min((int64_t)wgs, units)}; }
 
 }  // namespace eldr

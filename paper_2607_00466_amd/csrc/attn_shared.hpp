@@ -10,10 +10,8 @@
 // the matrix cores use it up, and the tile is no larger than it has to be, since
 // each workgroup leaves a part of every row it held.
 //
-// The softmax is as in the other kernel: S^T = K Q^T, weights used where the
-// product left them.  Its maximum is taken of the raw scores and the scale
-// enters the exponent's multiply-add (a negative scale is turned into a
-// positive one by the sign of q).
+// The products and the softmax are as in the other kernel: S^T = K Q^T, weights
+// used where the product left them.
 #pragma once
 
 #include "attn_plan.hpp"
@@ -34,6 +32,7 @@ struct SharedTile {
   static constexpr int kChunks = D / 8;                   // 16-byte pieces of a row in LDS
   static constexpr int kPieces = kStage * kChunks / kSharedThreads;  // a thread stages, of keys and of values
   static constexpr int kStageBytes = kStage * D * 2;      // of one cache
+  static constexpr int kAhead = D == 256 ? 1 : 2;         // stages in flight
   static constexpr int kMergeWords = kQ * (D / 16 * 4 + 2);
   static constexpr int kBytes = 4 * kStageBytes > kRowWaves * kMergeWords * kWave * 4 ? 4 * kStageBytes
                                                                                       : kRowWaves * kMergeWords * kWave * 4;
@@ -45,30 +44,32 @@ struct SharedTile {
   }
 };
 
-// A thread's share of one stage of one cache, on its way from HBM to LDS.
+// A thread's share of one stage of one cache, on its way from HBM to LDS.  Wave
+// w stages slots [8 w, 8 w + 8), half of a 16-slot tile, so all in one page:
+// pass i's piece is piece lane % kChunks of slot 8 w + lane / kChunks + i kRowsPass.
 template <int D, bool FP8>
 struct Piece {
   using S = SharedTile<D>;
   typedef typename std::conditional<FP8, u32x2, u32x4>::type Raw;
+  static constexpr int kElem = FP8 ? 1 : 2;
+  static constexpr int kRowsPass = kWave / S::kChunks;
   Raw raw[S::kPieces];
-  __device__ __forceinline__ void load(const char* const (&rows)[S::kPieces], const bool (&ok)[S::kPieces], uint32_t off) {
+  __device__ __forceinline__ void load(const char* tile, uint32_t off) {
 #pragma unroll
-    for (int i = 0; i < S::kPieces; ++i) {
-      Raw x = {};
-      if (ok[i]) x = *reinterpret_cast<const Raw*>(rows[i] + off);
-      raw[i] = x;
-    }
+    for (int i = 0; i < S::kPieces; ++i) raw[i] = *reinterpret_cast<const Raw*>(tile + off + i * kRowsPass * D * kElem);
   }
-  __device__ __forceinline__ void store(char* lds) const {
+  // live: the lane's slots that count come before it (of pass i: before live - i kRowsPass)
+  __device__ __forceinline__ void store(char* stage, const uint32_t (&at)[S::kPieces], bool whole, int live) const {
 #pragma unroll
     for (int i = 0; i < S::kPieces; ++i) {
-      const int p = threadIdx.x + i * kSharedThreads;
       u32x4 x;
       if constexpr (FP8)
         x = u32x4{fp8_pair<false>(raw[i][0]), fp8_pair<true>(raw[i][0]), fp8_pair<false>(raw[i][1]), fp8_pair<true>(raw[i][1])};
       else
         x = raw[i];
-      *reinterpret_cast<u32x4*>(lds + S::at(p / S::kChunks, p % S::kChunks)) = x;
+      // slots that do not count become zeros: their bits may be NaN
+      if (!whole) x = keep_if(i * kRowsPass < live, x);
+      *reinterpret_cast<u32x4*>(stage + at[i]) = x;
     }
   }
 };
@@ -98,9 +99,7 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int half = wave / kRowWaves, wave_row = sg.row0 + wave % kRowWaves * S::kQ * kRows;
   const bool live = wave_row < sg.rows;  // the wave has rows
-  const float unit0 = a.scale * kLog2e * (FP8 && a.k_scale ? a.k_scale[sg.h] : 1.0f);
-  const float unit = fabsf(unit0);
-  const uint32_t flip = unit0 < 0.0f ? 0x80008000u : 0u;
+  const float unit = a.scale * kLog2e * (FP8 && a.k_scale ? a.k_scale[sg.h] : 1.0f);
   u32x4 q[S::kQ][kK];
 #pragma unroll
   for (int t = 0; t < S::kQ; ++t) {
@@ -111,10 +110,10 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
 #pragma unroll
     for (int s = 0; s < kK; ++s) {
       const u32x4 x = *reinterpret_cast<const u32x4*>(src + s * 32 + g * 8);
-      q[t][s] = there ? x ^ flip : u32x4{0u, 0u, 0u, 0u};
+      q[t][s] = keep_if(there, x);
     }
   }
-  float m[S::kQ], l[S::kQ];  // maximum (raw) and this lane's part of the sum of row n
+  float m[S::kQ], l[S::kQ];  // reference, and this lane's part of the sum, of row n
   f32x4 acc[S::kQ][kV];
 #pragma unroll
   for (int t = 0; t < S::kQ; ++t) {
@@ -123,41 +122,69 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
     for (int c = 0; c < kV; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const int32_t* table = pg.table + (int64_t)sg.table_row * pg.max_blocks;
-  // the rows that this wave stages in pass i lie in one 16-slot tile, so in one page
-  constexpr int kRowsPass = kSharedThreads / S::kChunks, kRowsWave = kWave / S::kChunks;
-  const int in_row = (threadIdx.x % S::kChunks) * 8 * kElem;
-  const int row_in_wave = lane / S::kChunks;
-  Piece<D, FP8> next_k, next_v;
-  const auto fetch = [&](int k) {
-    const char *kp[S::kPieces], *vp[S::kPieces];
-    bool ok[S::kPieces];
+  // stage i on its way: set i % kAhead
+  Piece<D, FP8> next_k[S::kAhead], next_v[S::kAhead];
+  const int my_row = lane / S::kChunks;  // of the wave's eight, in pass 0
+  const uint32_t off = (uint32_t)((wave % 2 * 8 + my_row) * D + lane % S::kChunks * 8) * kElem;
+  uint32_t put[S::kPieces];
 #pragma unroll
-    for (int i = 0; i < S::kPieces; ++i) {
-      const int first = k + i * kRowsPass + wave * kRowsWave;  // the wave's first row: a slot
-      const int page = first < sg.k1 ? table[first >> pg.shift] : -1;
-      const bool has = pg.has(page);
-      const int64_t at = pg.row(has ? page : 0, sg.h, first) * kElem;
-      kp[i] = a.k_cache + at;
-      vp[i] = a.v_cache + at;
-      ok[i] = has && first + row_in_wave < sg.k1;
-    }
-    const uint32_t off = (uint32_t)(row_in_wave * D * kElem + in_row);
-    next_k.load(kp, ok, off);
-    next_v.load(vp, ok, off);
+  for (int i = 0; i < S::kPieces; ++i) put[i] = S::at(wave * 8 + my_row + i * Piece<D, FP8>::kRowsPass, lane % S::kChunks);
+  // The pages of 64 16-slot tiles (a window), lane i the i-th's, asked for one
+  // window ahead: a scalar load a stage would be waited for with every LDS read.
+  // present[w % 2]: which tiles of window w count and have a page.
+  constexpr int kWindow = kWave * 16;
+  const auto look_up = [&](int window) {
+    const int slot = window * kWindow + lane * 16;
+    return slot < sg.k1 ? table[slot >> pg.shift] : -1;
   };
-  char* stage = lds;
-  fetch(sg.k0);
-  next_k.store(stage);
-  next_v.store(stage + S::kStageBytes);
+  int pages = look_up(sg.k0 / kWindow), pages_next = look_up(sg.k0 / kWindow + 1);
+  uint64_t present[2];
+  present[0] = present[1] = __ballot(pg.has(pages));
+  // which of stage k's four tiles are there
+  const auto tiles_there = [&](int k) { return (uint32_t)(present[k / kWindow % 2] >> (k / 16 % kWave)) & 15u; };
+  const int64_t head_at = (int64_t)sg.h << pg.shift;
+  const int in_page = (1 << pg.shift) - 1;
+  const auto fetch = [&](int set, int k) {
+    if (k % kWindow == 0 && k != sg.k0) {
+      pages = pages_next;
+      pages_next = look_up(k / kWindow + 1);
+      present[k / kWindow % 2] = __ballot(pg.has(pages));
+    }
+    const int slot = k + wave / 2 * 16;
+    int page = __builtin_amdgcn_readlane(pages, slot / 16 % kWave);
+    page = pg.has(page) ? page : 0;
+    const int64_t at = (page * pg.block_stride + (head_at + (slot & in_page)) * D) * kElem;
+    next_k[set].load(a.k_cache + at, off);
+    next_v[set].load(a.v_cache + at, off);
+  };
+  // stage k from its set to the buffer
+  const auto store = [&](int set, int k, char* to) {
+    const uint32_t there = tiles_there(k);
+    const bool whole = there == 15u && k + kStage <= sg.k1;
+    const int live = (there >> (wave / 2) & 1u) ? sg.k1 - (k + wave * 8 + my_row) : 0;
+    next_k[set].store(to, put, whole, live);
+    next_v[set].store(to + S::kStageBytes, put, whole, live);
+  };
+  // where the lane's operands lie in a stage (the swizzle repeats every 16 rows)
+  uint32_t k_at[kK], v_at[4];
+#pragma unroll
+  for (int i = 0; i < kK; ++i) k_at[i] = S::at(half * kStep + n, i * 4 + g);
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    v_at[j] = S::kStageBytes + (D == 64 ? S::at(half * kStep + 4 * g + j, n / 2) + (n % 2) * 8
+                                        : S::at(half * kStep + 4 * g + j, n * (kV / 8)));
+  constexpr uint32_t kTileBytes = kRows * D * 2;  // 16 slots
+#pragma unroll
+  for (int i = 0; i < S::kAhead; ++i)
+    if (sg.k0 + i * kStage < sg.k1) fetch(i, sg.k0 + i * kStage);
+  store(0, sg.k0, lds);
   __syncthreads();
-  for (int k = sg.k0; k < sg.k1; k += kStage) {
-    char* other = lds + (stage == lds ? 2 * S::kStageBytes : 0);
-    const bool more = k + kStage < sg.k1;
-    if (more) fetch(k + kStage);
+  // one stage: k's slots lie in buffer `stage`; set (of k) is free again
+  const auto use = [&](int k, int set, int next_set, char* stage, char* other) {
+    if (k + S::kAhead * kStage < sg.k1) fetch(set, k + S::kAhead * kStage);
     const int k_mine = k + half * kStep;
+    const uint32_t there = tiles_there(k) >> (2 * half);
     if (live && k_mine < sg.k1) {
-      const char *ks = stage, *vs = stage + S::kStageBytes;
-      const int r0 = half * kStep;
       f32x4 s[S::kQ][2];
 #pragma unroll
       for (int t = 0; t < S::kQ; ++t) s[t][0] = s[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -165,46 +192,20 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
       for (int i = 0; i < kK; ++i) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          const u32x4 x = *reinterpret_cast<const u32x4*>(ks + S::at(r0 + 16 * b + n, i * 4 + g));
+          const u32x4 x = *reinterpret_cast<const u32x4*>(stage + k_at[i] + b * kTileBytes);
 #pragma unroll
           for (int t = 0; t < S::kQ; ++t) s[t][b] = mfma16x16x32(x, q[t][i], s[t][b]);
         }
       }
-      const int next = (k_mine + 16) >> pg.shift;
-      const bool has0 = pg.has(table[k_mine >> pg.shift]), has1 = next < pg.max_blocks && pg.has(table[next]);
-      if (!(has0 && has1 && k_mine + kStep <= sg.k1)) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const bool keep = (j < 4 ? has0 : has1) && k_mine + (j / 4) * 16 + 4 * g + j % 4 < sg.k1;
-#pragma unroll
-          for (int t = 0; t < S::kQ; ++t) s[t][j / 4][j % 4] = keep ? s[t][j / 4][j % 4] : -INFINITY;
-        }
-      }
+      const bool whole = (there & 3u) == 3u && k_mine + kStep <= sg.k1;
+      const auto keep = [&](int j) { return (there >> (j / 4) & 1u) && k_mine + (j / 4) * 16 + 4 * g + j % 4 < sg.k1; };
       u32x4 p[S::kQ];
 #pragma unroll
-      for (int t = 0; t < S::kQ; ++t) {
-        float top = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])),
-                          fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        if (__any(top > m[t])) {
-          const float m2 = fmaxf(m[t], top);
-          const float back = m2 == -INFINITY ? 0.0f : exp2_fast((m[t] - m2) * unit);
-          m[t] = m2;
-          l[t] *= back;
+      for (int t = 0; t < S::kQ; ++t)
+        p[t] = softmax_step(s[t], unit, whole, keep, m[t], l[t], [&](float f) {
 #pragma unroll
-          for (int c = 0; c < kV; ++c) acc[t][c] *= back;
-        }
-        const float base = m[t] == -INFINITY ? 0.0f : m[t] * unit;
-        float x[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          x[j] = exp2_fast(fmaf(s[t][j / 4][j % 4], unit, -base));
-          l[t] += x[j];
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[t][i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-      }
+          for (int c = 0; c < kV; ++c) acc[t][c] *= f;
+        });
       // eight value columns a lane at a time (four where D is 64)
       constexpr int kCols = kV < 8 ? kV : 8;
 #pragma unroll
@@ -212,12 +213,13 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
         Values<kCols * 16, false> v;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int r = r0 + (j / 4) * 16 + 4 * g + j % 4;
+          // (neighbouring pieces of a row differ in the lowest bit of their place)
+          const char* from = stage + ((v_at[j % 4] ^ (w * 16)) + (j / 4) * kTileBytes);
           if constexpr (D == 64) {
-            const u32x2 x = *reinterpret_cast<const u32x2*>(vs + S::at(r, n / 2) + (n % 2) * 8);
+            const u32x2 x = *reinterpret_cast<const u32x2*>(from);
             v.raw[j][0] = x[0], v.raw[j][1] = x[1];
           } else {
-            const u32x4 x = *reinterpret_cast<const u32x4*>(vs + S::at(r, n * (kV / 8) + w));
+            const u32x4 x = *reinterpret_cast<const u32x4*>(from);
 #pragma unroll
             for (int i = 0; i < 4; ++i) v.raw[j][i] = x[i];
           }
@@ -230,53 +232,70 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
         }
       }
     }
-    if (more) {
-      next_k.store(other);
-      next_v.store(other + S::kStageBytes);
-    }
-    stage = other;
+    if (k + kStage < sg.k1) store(next_set, k + kStage, other);
     __syncthreads();
+  };
+  char* const buffers[2] = {lds, lds + 2 * S::kStageBytes};
+  for (int k = sg.k0; k < sg.k1; k += 2 * kStage) {
+    use(k, 0, 1 % S::kAhead, buffers[0], buffers[1]);
+    if (k + kStage < sg.k1) use(k + kStage, 1 % S::kAhead, 0, buffers[1], buffers[0]);
   }
-  // the second half's waves hand their state to the first half's, lane by lane
-  float* swap = reinterpret_cast<float*>(lds) + (wave % kRowWaves) * S::kMergeWords * kWave + lane;
-  if (half == 1) {
+  // The halves add up: each hands the other the row tile that it does not finish
+  // (tile t is finished by half t; with one tile the second half only hands over),
+  // lane by lane.
+  const auto spot = [&](int t) {
+    return reinterpret_cast<float*>(lds) + (wave % kRowWaves * S::kQ + t) * (kV * 4 + 2) * kWave + lane;
+  };
 #pragma unroll
-    for (int t = 0; t < S::kQ; ++t) {
-      float* to = swap + t * (kV * 4 + 2) * kWave;
-      to[0] = m[t], to[kWave] = l[t];
+  for (int t = 0; t < S::kQ; ++t) {
+    if (t == half) continue;
+    float* to = spot(t);
+    to[0] = m[t], to[kWave] = l[t];
 #pragma unroll
-      for (int c = 0; c < kV; ++c)
+    for (int c = 0; c < kV; ++c)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) to[(2 + c * 4 + i) * kWave] = acc[t][c][i];
-    }
+      for (int i = 0; i < 4; ++i) to[(2 + c * 4 + i) * kWave] = acc[t][c][i];
   }
   __syncthreads();
-  if (half == 0 && live) {
+  f32x4 sum[kV];
+  float top = -INFINITY, total = 0.0f;
 #pragma unroll
-    for (int t = 0; t < S::kQ; ++t) {
-      const float* from = swap + t * (kV * 4 + 2) * kWave;
-      const float m1 = from[0], m2 = fmaxf(m[t], m1);
-      const bool none = m2 == -INFINITY;
-      const float f0 = none ? 0.0f : exp2_fast((m[t] - m2) * unit), f1 = none ? 0.0f : exp2_fast((m1 - m2) * unit);
-      float sum = l[t] * f0 + from[kWave] * f1;
-      sum += __shfl_xor(sum, 16);
-      sum += __shfl_xor(sum, 32);
-      const int row = wave_row + t * kRows + n;
-      if (row < sg.rows) {
-        const int64_t q_row = (int64_t)(sg.table_row + row / a.G) * a.Hq + sg.h * a.G + row % a.G;
-        float* to = part + (by_row ? q_row : (int64_t)(row - sg.row0)) * (D + 4);
+  for (int t = 0; t < S::kQ; ++t) {
+    if (t != half) continue;
+    const float* from = spot(t);
+    const float m1 = from[0];
+    top = fmaxf(m[t], m1);
+    const bool none = top == -INFINITY;
+    const float f0 = none ? 0.0f : exp2_fast(m[t] - top), f1 = none ? 0.0f : exp2_fast(m1 - top);
+    total = l[t] * f0 + from[kWave] * f1;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+    for (int c = 0; c < kV; ++c)
 #pragma unroll
-          for (int c = 0; c < kV; c += 4) {
-            f32x4 x;
+      for (int i = 0; i < 4; ++i) sum[c][i] = acc[t][c][i] * f0 + from[(2 + c * 4 + i) * kWave] * f1;
+  }
+  total += __shfl_xor(total, 16);
+  total += __shfl_xor(total, 32);
+  __syncthreads();
+  // through LDS once more, so that the parts are written as whole lines
+  constexpr int kPitch = D + 4;
+  float* tile = reinterpret_cast<float*>(lds);
+  if (half < S::kQ) {
+    float* row = tile + (wave % kRowWaves * S::kQ * kRows + half * kRows + n) * kPitch;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = acc[t][c + e][i] * f0 + from[(2 + (c + e) * 4 + i) * kWave] * f1;
-            *reinterpret_cast<f32x4*>(to + (4 * g + i) * kV + c) = x;
-          }
-        if (g == 0) to[D] = none ? -INFINITY : m2 * unit, to[D + 1] = sum;
-      }
-    }
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < kV; c += 4)
+        *reinterpret_cast<f32x4*>(row + (4 * g + i) * kV + c) = f32x4{sum[c][i], sum[c + 1][i], sum[c + 2][i], sum[c + 3][i]};
+    if (g == 0) *reinterpret_cast<f32x4*>(row + D) = f32x4{top, total, 0.0f, 0.0f};
+  }
+  __syncthreads();
+  constexpr int kQuads = kPitch / 4;
+  const int live_rows = min(S::kRowsWg, sg.rows - sg.row0);
+  for (int e = threadIdx.x; e < live_rows * kQuads; e += kSharedThreads) {
+    const int r = e / kQuads, row = sg.row0 + r;
+    const int64_t q_row = (int64_t)(sg.table_row + row / a.G) * a.Hq + sg.h * a.G + row % a.G;
+    *reinterpret_cast<f32x4*>(part + (by_row ? q_row : (int64_t)r) * kPitch + (e - r * kQuads) * 4) =
+        *reinterpret_cast<const f32x4*>(tile + e * 4);
   }
   __syncthreads();
 }
@@ -289,10 +308,11 @@ __global__ __launch_bounds__(kSharedThreads, 2) void attn_shared_kernel(SharedAr
   const int capacity = pg.capacity();
   const Plan plan = make_plan<kSharedThreads>(a.gr, capacity, a.G, S::kRowsWg, reinterpret_cast<int*>(lds_shared + S::kBytes), waves);
   const int R = a.gr.R, n = a.gr.n, row = plan.shared[n];
-  const Deal deal = deal_of((int64_t)row * pg.Hkv, kSharedWgs);
-  if ((int)blockIdx.x >= deal.wgs) return;
-  int u = __builtin_amdgcn_readfirstlane(deal.first(blockIdx.x));
-  const int end = __builtin_amdgcn_readfirstlane(deal.first(blockIdx.x + 1));
+  const Deal deal(row * pg.Hkv, kSharedWgs);
+  const int w = (int)blockIdx.x % kNumXcd * (kSharedWgs / kNumXcd) + (int)blockIdx.x / kNumXcd;
+  if (w >= deal.wgs) return;
+  int u = __builtin_amdgcn_readfirstlane(deal.first(w));
+  const int end = __builtin_amdgcn_readfirstlane(deal.first(w + 1));
   while (u < end) {
     const int h = u / row, v = u - h * row;
     const int grp = last_at(plan.shared, n, v);
@@ -306,7 +326,7 @@ __global__ __launch_bounds__(kSharedThreads, 2) void attn_shared_kernel(SharedAr
     for (int i = 0; i < (int)(sizeof(sg) / 4); ++i) f[i] = __builtin_amdgcn_readfirstlane(f[i]);
     const bool begins = sg.k0 == 0;
     attend_shared<D, FP8>(a, pg, sg, lds_shared,
-                          begins ? a.rows_part : a.rest_part + (int64_t)blockIdx.x * S::kRowsWg * (D + 4), begins);
+                          begins ? a.rows_part : a.rest_part + (int64_t)w * S::kRowsWg * (D + 4), begins);
     u += tiles;
   }
 }

@@ -30,6 +30,23 @@ __device__ __forceinline__ uint32_t fp8_pair(uint32_t w) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
 }
 
+// v, or zeros: a mask, so that the load that gave v stays where it is (a select
+// would move it behind a branch).
+__device__ __forceinline__ u32x4 keep_if(bool keep, u32x4 v) { return v & (keep ? 0xffffffffu : 0u); }
+
+// The two pages of a 32-slot step that starts at slot k, a multiple of kStep;
+// -1 past the table.  table: one request's row.
+struct StepPages {
+  int b0, b1;
+};
+__device__ __forceinline__ StepPages step_pages(const Pages& pg, const int32_t* table, int k) {
+  const int i0 = k >> pg.shift, i1 = (k + 16) >> pg.shift, last = pg.max_blocks - 1;
+  StepPages s{uniform_load(table + min(i0, last)), uniform_load(table + min(i1, last))};
+  if (i0 > last) s.b0 = -1;
+  if (i1 > last) s.b1 = -1;
+  return s;
+}
+
 // One 16-slot tile of keys as MFMA operands.
 template <int D, bool FP8>
 struct Keys {
@@ -102,5 +119,61 @@ struct Values {
     return v;
   }
 };
+
+// The larger of the four lanes that hold one query row (lane % 16), in all of them.
+__device__ __forceinline__ float row_max(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// How far (in powers of two) a score may lie over the reference before the
+// reference moves: weights of up to 2^8 cost fp32 and bf16 nothing, and a
+// reference that stands still costs no exchange between lanes and no rescaling.
+constexpr float kSlack = 8.0f;
+
+// One step of the softmax of query row lane % 16 over the lane's 8 of 32 slots:
+// the weights exp2(unit s - m) as the second product's operand.  m: the row's
+// reference (-inf before the first slot that counts); l: this lane's part of the
+// sum, of the weights in 32 bits; keep(j): slot j counts (asked unless `whole`);
+// rescale(f): called, for all lanes, when the sums so far become f times as much.
+template <typename Keep, typename Rescale>
+__device__ __forceinline__ u32x4 softmax_step(const f32x4 (&s)[2], float unit, bool whole, Keep keep, float& m, float& l,
+                                              Rescale rescale) {
+  float e[8];
+  // the largest in the branch that makes the exponents: after a merge the
+  // compiler no longer knows them to be quiet and adds an instruction for each
+  const auto largest = [&] { return fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(e[0], e[1]), e[2]), e[3]), e[4]), e[5]), e[6]), e[7]); };
+  const auto exponents = [&](float base) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = fmaf(s[j / 4][j % 4], unit, -base);
+    if (whole) return largest();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = keep(j) ? e[j] : -INFINITY;
+    return largest();
+  };
+  const bool none = m == -INFINITY;
+  const float base = none ? 0.0f : m;
+  const float top = exponents(base);
+  if (__any(top > (none ? -INFINITY : kSlack))) {
+    const float m2 = fmaxf(m, base + row_max(top));
+    const float back = m2 == -INFINITY ? 1.0f : exp2_fast(m - m2);
+    m = m2;
+    l *= back;
+    rescale(back);
+    exponents(m2 == -INFINITY ? 0.0f : m2);
+  }
+  u32x4 p;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    e[j] = exp2_fast(e[j]);
+    l += e[j];
+  }
+  // rounded to bf16 for the product alone: the sum keeps 32 bits
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = pack_bf16(e[2 * i], e[2 * i + 1]);
+  return p;
+}
 
 }  // namespace eldr

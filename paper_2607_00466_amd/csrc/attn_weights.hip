@@ -69,10 +69,11 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
   f32x4 lse;
   const bool once = sp.row1 - sp.row0 <= kRows;  // one tile of rows: its operands stay
   if (once) load_rows<D, FP8>(a, sp, sp.row0, q, lse);
-  for (int k = sp.k0 / kStep * kStep + wave * kStep; k < sp.k1; k += kWeightWaves * kStep) {
-    const int b0 = table[k >> pg.shift];
-    const int next = (k + 16) >> pg.shift;
-    const int b1 = next < pg.max_blocks ? table[next] : -1;
+  const int k_first = sp.k0 / kStep * kStep + wave * kStep;
+  StepPages pages = step_pages(pg, table, k_first);  // one step ahead
+  for (int k = k_first; k < sp.k1; k += kWeightWaves * kStep) {
+    const int b0 = pages.b0, b1 = pages.b1;
+    pages = step_pages(pg, table, k + kWeightWaves * kStep);
     const bool has0 = pg.has(b0), has1 = pg.has(b1);
     Keys<D, FP8> keys[2];
     keys[0].load(a.k_cache + pg.row(has0 ? b0 : 0, sp.h, k) * T::kElem, n, g);
@@ -130,26 +131,27 @@ __global__ __launch_bounds__(kWeightThreads, D == 256 ? 3 : 4) void attn_weights
   const int R = a.gr.R, n = a.gr.n, wgs = gridDim.x;
   const int own_row = plan.own[R], shared_row = plan.shared[n];
   // one line: the shared units, then the own ones
-  const int64_t shared_units = (int64_t)shared_row * pg.Hkv, units = shared_units + (int64_t)own_row * pg.Hkv;
-  int64_t u = (int64_t)blockIdx.x * units / wgs;
-  const int64_t end = (int64_t)(blockIdx.x + 1) * units / wgs;
+  const int shared_units = shared_row * pg.Hkv;
+  const Deal deal(shared_units + own_row * pg.Hkv, wgs);
+  if ((int)blockIdx.x >= deal.wgs) return;
+  int u = __builtin_amdgcn_readfirstlane(deal.first(blockIdx.x));
+  const int end = __builtin_amdgcn_readfirstlane(deal.first(blockIdx.x + 1));
   while (u < end) {
     Span sp;
     int tiles;
     if (u < shared_units) {
-      const int h = (int)(u / shared_row), v = (int)(u - (int64_t)h * shared_row);
+      const int h = u / shared_row, v = u - h * shared_row;
       const int grp = last_at(plan.shared, n, v);
       const int first = max(a.gr.start[grp], 0), last = min(a.gr.start[grp + 1], R), reach = plan.least[grp];
       const int per = tiles_of(0, reach), in = v - plan.shared[grp], run = in / per, t = in - run * per;
-      tiles = (int)min((int64_t)(per - t), end - u);
+      tiles = min(per - t, end - u);
       sp = Span{first, first, last, grp, run * member_rows, min((run + 1) * member_rows, (last - first) * a.pad), h,
                 t * kTile, min((t + tiles) * kTile, reach)};
     } else {
-      const int64_t o = u - shared_units;
-      const int h = (int)(o / own_row), v = (int)(o - (int64_t)h * own_row);
+      const int o = u - shared_units, h = o / own_row, v = o - h * own_row;
       const int r = last_at(plan.own, R, v), t = v - plan.own[r];
       const int len = clamp_len(a.gr.lens[r], capacity), lo = min(plan.reach[r], len), t0 = lo / kTile;
-      tiles = (int)min((int64_t)(plan.own[r + 1] - v), end - u);
+      tiles = min(plan.own[r + 1] - v, end - u);
       sp = Span{r, r, r + 1, -1, 0, a.pad, h, max((t0 + t) * kTile, lo), min((t0 + t + tiles) * kTile, len)};
     }
     // the same for every lane: keep it in scalar registers
