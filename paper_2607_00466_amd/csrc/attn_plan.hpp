@@ -35,17 +35,6 @@ struct Plan {
   static __host__ __device__ size_t bytes(int R, int n) { return sizeof(int) * (3 * (size_t)R + 1 + 2 * (size_t)n + 1); }
 };
 
-// Inclusive sum over a wave's lanes.
-__device__ __forceinline__ int wave_sum_before(int v) {
-  const int lane = threadIdx.x % kWave;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int y = __shfl_up(v, o);
-    if (lane >= o) v += y;
-  }
-  return v;
-}
-
 // out[0] = 0, out[i + 1] = sum of f(0 .. i), by THREADS threads, i ascending a thread.
 template <int THREADS, typename F>
 __device__ __forceinline__ void sums(int n, int* out, int* waves, F f) {
