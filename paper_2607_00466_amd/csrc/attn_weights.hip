@@ -9,9 +9,10 @@
 // requests: G is padded to a power of two (or to a multiple of 16), and a padded
 // row's lse of +inf makes its weights zero.
 //
-// A wave takes 32 slots at a time; a unit is 128 slots of one request, or of a
-// group against a run of its members' rows, dealt out as for moe_attn_decode.
-// Bound by HBM: keys once, weights in and out.
+// A unit is 128 slots of one request, or of a group against up to kMemberTiles
+// tiles of its members' rows, dealt out as for moe_attn_decode.  A wave keeps its
+// rows' queries and lse in registers and takes 32 slots at a time, the next ones'
+// keys on their way.  Bound by HBM: keys once, weights in and out.
 #include "attn_plan.hpp"
 #include "attn_tile.hpp"
 
@@ -19,8 +20,11 @@ namespace eldr {
 
 constexpr int kWeightThreads = 256;
 constexpr int kWeightWaves = kWeightThreads / kWave;
-constexpr int kWeightWgs = 1024;  // four for each CU
-constexpr int kMemberRows = 64;   // rows of a shared unit, of requests of up to 16 rows
+constexpr int kWeightWgs = 512;  // two for each CU
+
+// Row tiles of a shared unit, for requests of up to 16 rows: as many as a wave
+// keeps in registers beside a lane's requests in each, 4 / pad.
+constexpr int member_tiles(int D, int pad) { return pad == 1 ? 1 : pad == 2 || D == 256 ? 2 : 4; }
 
 struct WeightArgs {
   const uint16_t* q;
@@ -55,7 +59,30 @@ __device__ __forceinline__ void load_rows(const WeightArgs& a, const Span& sp, i
   }
 }
 
-template <int D, bool FP8>
+// exp2(unit s - lse), added to the rows' weights.
+__device__ __forceinline__ void add_weights(const f32x4& s, float unit, const f32x4& lse, f32x4& sum) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c) sum[c] += exp2_fast(fmaf(s[c], unit, -lse[c]));
+}
+
+// The sums over the `in_tile` rows of each request of a 16-row tile: in element
+// c of the lanes whose row 4 (lane / 16) + c is a request's first.
+__device__ __forceinline__ void sum_heads(f32x4& x, int in_tile) {
+  if (in_tile >= 2) x[0] += x[1], x[2] += x[3];
+  if (in_tile >= 4) x[0] += x[2];
+  if (in_tile >= 8) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[0]), __float_as_uint(x[0]), false, false);
+    x[0] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  }
+  if (in_tile >= 16) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[0]), __float_as_uint(x[0]), false, false);
+    x[0] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  }
+}
+
+// The tiles of rows from sp.row0 on, of requests of up to 16 rows; a lane has up
+// to PER requests in a tile, every 4 / PER-th of its rows.
+template <int D, bool FP8, int TILES, int PER>
 __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, const Span& sp, const int* group) {
   using T = Tile<D, FP8>;
   const int lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
@@ -63,67 +90,143 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
   const float unit = a.scale * kLog2e * (FP8 && a.k_scale ? a.k_scale[sp.h] : 1.0f);
   const int32_t* table = pg.table + (int64_t)sp.table_row * pg.max_blocks;
   const int64_t N = pg.capacity();
-  const int in_tile = min(a.pad, kRows);       // rows of one request in a tile
-  const int per_request = (a.pad + kRows - 1) / kRows;  // tiles of one request
-  u32x4 q[T::kK];
-  f32x4 lse;
-  const bool once = sp.row1 - sp.row0 <= kRows;  // one tile of rows: its operands stay
-  if (once) load_rows<D, FP8>(a, sp, sp.row0, q, lse);
-  const int k_first = sp.k0 / kStep * kStep + wave * kStep;
-  StepPages pages = step_pages(pg, table, k_first);  // one step ahead
-  for (int k = k_first; k < sp.k1; k += kWeightWaves * kStep) {
-    const int b0 = pages.b0, b1 = pages.b1;
-    pages = step_pages(pg, table, k + kWeightWaves * kStep);
-    const bool has0 = pg.has(b0), has1 = pg.has(b1);
+  constexpr int kEach = 4 / PER;
+  const int64_t next_request = (int64_t)pg.Hkv * N;
+  u32x4 q[TILES][T::kK];
+  f32x4 lse[TILES];
+  int64_t at[TILES];    // of the lane's first request's weights, at slot 0
+  uint32_t mine = 0;    // bit PER t + c: the lane writes its c-th request of tile t
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) {
+    const int row0 = sp.row0 + t * kRows;
+    load_rows<D, FP8>(a, sp, row0, q[t], lse[t]);
+    const int first = sp.first + (row0 + 4 * g) / a.pad;
+    at[t] = ((int64_t)first * pg.Hkv + sp.h) * N;
+#pragma unroll
+    for (int c = 0; c < PER; ++c) {
+      const int row = row0 + 4 * g + c * kEach, r = sp.first + row / a.pad;
+      if (row % a.pad == 0 && row < sp.row1 && r < sp.end && (sp.group < 0 || group[r] == sp.group)) mine |= 1u << (PER * t + c);
+    }
+  }
+  // Steps are asked for kAhead before they are used: keys, and the weights so far.
+  constexpr int kAhead = TILES == 1 ? (D == 256 ? 2 : 3) : (D == 256 ? 1 : 2);
+  constexpr int kStride = kWeightWaves * kStep;
+  struct Set {
     Keys<D, FP8> keys[2];
-    keys[0].load(a.k_cache + pg.row(has0 ? b0 : 0, sp.h, k) * T::kElem, n, g);
-    keys[1].load(a.k_cache + pg.row(has1 ? b1 : 0, sp.h, k + 16) * T::kElem, n, g);
-    const bool write[2] = {k + n >= sp.k0 && k + n < sp.k1, k + 16 + n >= sp.k0 && k + 16 + n < sp.k1};
-    for (int row0 = sp.row0; row0 < sp.row1; row0 += kRows * per_request) {
-      // what is there already, asked for with the keys
-      float before[2][4];
-      int64_t at[4];
-      bool mine[4];
+    float before[TILES][2][PER];
+    StepPages pages;
+  } sets[kAhead];
+  const int k_first = sp.k0 / kStep * kStep + wave * kStep;
+  StepPages pages = step_pages(pg, table, k_first);  // of the next step to be asked for
+  const auto counts = [&](int slot) { return slot >= sp.k0 && slot < sp.k1; };
+  const auto fetch = [&](Set& s, int k) {
+    s.pages = pages;
+    pages = step_pages(pg, table, k + kStride);
+    if (k >= sp.k1) return;
+    s.keys[0].load(a.k_cache + pg.row(pg.has(s.pages.b0) ? s.pages.b0 : 0, sp.h, k) * T::kElem, n, g);
+    s.keys[1].load(a.k_cache + pg.row(pg.has(s.pages.b1) ? s.pages.b1 : 0, sp.h, k + 16) * T::kElem, n, g);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int row = 4 * g + c, r = sp.first + (row0 + row) / a.pad;
-        mine[c] = (c == 0 || in_tile <= c) && row % in_tile == 0 && r < sp.end && (sp.group < 0 || group[r] == sp.group);
-        at[c] = ((int64_t)r * pg.Hkv + sp.h) * N + k + n;
+    for (int t = 0; t < TILES; ++t)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) before[t][c] = mine[c] && write[t] && a.weights_in ? a.weights_in[at[c] + 16 * t] : 0.0f;
+      for (int c = 0; c < PER; ++c) {
+        const float* from = a.weights_in + at[t] + c * next_request + k + n;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          float x = 0.0f;
+          if (a.weights_in && (mine >> (PER * t + c) & 1u) && counts(k + 16 * b + n)) x = from[16 * b];
+          s.before[t][b][c] = x;
+        }
       }
+  };
+  const auto use = [&](Set& st, int k) {
+    float sum[TILES][2][PER];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+      f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int i = 0; i < T::kK; ++i) {
+        s[0] = mfma16x16x32(q[t][i], st.keys[0].operand(i), s[0]);
+        s[1] = mfma16x16x32(q[t][i], st.keys[1].operand(i), s[1]);
+      }
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        add_weights(s[b], unit, lse[t], x);
+        sum_heads(x, a.pad);
+#pragma unroll
+        for (int c = 0; c < PER; ++c) sum[t][b][c] = x[c * kEach];
+      }
+    }
+    const bool there[2] = {pg.has(st.pages.b0), pg.has(st.pages.b1)};
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int c = 0; c < PER; ++c)
+          if ((mine >> (PER * t + c) & 1u) && counts(k + 16 * b + n))
+            a.weights_out[at[t] + c * next_request + k + n + 16 * b] = st.before[t][b][c] + (there[b] ? sum[t][b][c] : 0.0f);
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) fetch(sets[i], k_first + i * kStride);
+  for (int k = k_first; k < sp.k1; k += kAhead * kStride) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (k + i * kStride >= sp.k1) break;
+      use(sets[i], k + i * kStride);
+      fetch(sets[i], k + (i + kAhead) * kStride);
+    }
+  }
+}
+
+// The same for requests of more than 16 rows: tile by tile of one request, the
+// queries read again for every step.
+template <int D, bool FP8>
+__device__ __forceinline__ void weigh_wide(const WeightArgs& a, const Pages& pg, const Span& sp, const int* group) {
+  using T = Tile<D, FP8>;
+  const int lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const float unit = a.scale * kLog2e * (FP8 && a.k_scale ? a.k_scale[sp.h] : 1.0f);
+  const int32_t* table = pg.table + (int64_t)sp.table_row * pg.max_blocks;
+  const int64_t N = pg.capacity();
+  for (int k = sp.k0 / kStep * kStep + wave * kStep; k < sp.k1; k += kWeightWaves * kStep) {
+    const StepPages pages = step_pages(pg, table, k);
+    const bool there[2] = {pg.has(pages.b0), pg.has(pages.b1)};
+    Keys<D, FP8> keys[2];
+    keys[0].load(a.k_cache + pg.row(there[0] ? pages.b0 : 0, sp.h, k) * T::kElem, n, g);
+    keys[1].load(a.k_cache + pg.row(there[1] ? pages.b1 : 0, sp.h, k + 16) * T::kElem, n, g);
+    for (int row0 = sp.row0; row0 < sp.row1; row0 += a.pad) {
+      const int r = sp.first + row0 / a.pad;
+      if (r >= sp.end || (sp.group >= 0 && group[r] != sp.group)) continue;
       f32x4 sum[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-      for (int part = 0; part < per_request; ++part) {
-        if (!once) load_rows<D, FP8>(a, sp, row0 + part * kRows, q, lse);
+      for (int part = 0; part < a.pad; part += kRows) {
+        u32x4 q[T::kK];
+        f32x4 lse;
+        load_rows<D, FP8>(a, sp, row0 + part, q, lse);
         f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (int i = 0; i < T::kK; ++i) {
           s[0] = mfma16x16x32(q[i], keys[0].operand(i), s[0]);
           s[1] = mfma16x16x32(q[i], keys[1].operand(i), s[1]);
         }
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) sum[t][c] += exp2_fast(fmaf(s[t][c], unit, -lse[c]));
+        add_weights(s[0], unit, lse, sum[0]);
+        add_weights(s[1], unit, lse, sum[1]);
       }
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        float x[4] = {sum[t][0], sum[t][1], sum[t][2], sum[t][3]};
-        if (in_tile >= 2) x[0] += x[1], x[2] += x[3];
-        if (in_tile >= 4) x[0] += x[2];
-        if (in_tile >= 8) x[0] += __shfl_xor(x[0], 16);
-        if (in_tile >= 16) x[0] += __shfl_xor(x[0], 32);
-        const bool there = t ? has1 : has0;
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (mine[c] && write[t]) a.weights_out[at[c] + 16 * t] = before[t][c] + (there ? x[c] : 0.0f);
+      for (int b = 0; b < 2; ++b) {
+        sum_heads(sum[b], kRows);
+        const int slot = k + n + 16 * b;
+        if (g == 0 && slot >= sp.k0 && slot < sp.k1) {
+          const int64_t at = ((int64_t)r * pg.Hkv + sp.h) * N + slot;
+          a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.0f) + (there[b] ? sum[b][0] : 0.0f);
+        }
       }
     }
   }
 }
 
 template <int D, bool FP8>
-__global__ __launch_bounds__(kWeightThreads, D == 256 ? 3 : 4) void attn_weights_kernel(WeightArgs a, Pages pg, int member_rows) {
+__global__ __launch_bounds__(kWeightThreads, 2) void attn_weights_kernel(WeightArgs a, Pages pg, int member_rows) {
   extern __shared__ int lds[];
   __shared__ int waves[kWeightWaves];
   const int capacity = pg.capacity();
@@ -158,14 +261,18 @@ __global__ __launch_bounds__(kWeightThreads, D == 256 ? 3 : 4) void attn_weights
     int* f = reinterpret_cast<int*>(&sp);
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(sp) / 4); ++i) f[i] = __builtin_amdgcn_readfirstlane(f[i]);
-    weigh<D, FP8>(a, pg, sp, plan.group);
+    if (a.pad > kRows) weigh_wide<D, FP8>(a, pg, sp, plan.group);
+    else if (sp.group < 0) weigh<D, FP8, 1, 1>(a, pg, sp, plan.group);
+    else if (a.pad == 1) weigh<D, FP8, member_tiles(D, 1), 4>(a, pg, sp, plan.group);
+    else if (a.pad == 2) weigh<D, FP8, member_tiles(D, 2), 2>(a, pg, sp, plan.group);
+    else weigh<D, FP8, member_tiles(D, 4), 1>(a, pg, sp, plan.group);
     u += __builtin_amdgcn_readfirstlane(tiles);
   }
 }
 
 template <int D, bool FP8>
 int launch_weights(const WeightArgs& a, const Pages& pg, hipStream_t s) {
-  const int member_rows = a.pad > kRows ? a.pad : kMemberRows;
+  const int member_rows = a.pad > kRows ? a.pad : member_tiles(D, a.pad) * kRows;
   hipLaunchKernelGGL((attn_weights_kernel<D, FP8>), dim3(kWeightWgs), dim3(kWeightThreads), Plan::bytes(a.gr.R, a.gr.n), s, a,
                      pg, member_rows);
   return eldr_host::launch_status();
