@@ -1,11 +1,13 @@
 // moe_kv_append: rotary positions with any number of axes, fused with the
 // write of the new tokens' keys and values into the paged cache.
 //
-// One thread turns 16 values of one head of one token, i.e. the 8 pairs
-// [8c, 8c + 8) of its two half-heads (or of 16 neighbouring values where pairs
-// are interleaved), so every load and store is 16 bytes or more and both
-// values of a pair are in one thread.  Bound by bytes for a prompt and by two
-// dependent loads (position, then table) for a decode batch.
+// One thread turns 16 values of a head of a token, i.e. the 8 pairs [8c, 8c + 8)
+// of its two half-heads (or of 16 neighbouring values where pairs are
+// interleaved), so every load and store is 16 bytes or more and both values of a
+// pair are in one thread.  Where there are tokens enough to fill the chip, a
+// thread does so for several heads with the angles it has read once: a token's
+// angles are as many bytes as a head's values.  Bound by bytes for a prompt and
+// by two dependent loads (position, then table) for a decode batch.
 #include "attn_common.hpp"
 
 namespace eldr {
@@ -16,8 +18,9 @@ struct AppendArgs {
   const int32_t *positions, *pair_axis, *slots;
   const float *cos_table, *sin_table;
   uint16_t* q_out;
-  int64_t threads;  // T * heads * (D / 16)
+  int64_t threads;  // T * lanes * (D / 16)
   int32_t T, n_axes, max_pos, rot, Hq, heads, chunk_shift;
+  int32_t lanes;    // threads that share a token's heads
 };
 
 // Eight consecutive values as fp32.
@@ -81,72 +84,90 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(
   if (id >= a.threads) return;
   const int chunk = (int)(id & ((1 << a.chunk_shift) - 1));
   const int64_t th = id >> a.chunk_shift;
-  const int t = (int)(th / a.heads);
-  int h = (int)(th - (int64_t)t * a.heads);
-  // heads: the queries', the keys', the values'
-  const bool is_q = h < a.Hq, is_v = h >= a.Hq + pg.Hkv;
-  // (chosen by lane, so arguments of their own: fields of a struct would go to scratch)
-  const void* in = is_q ? q : is_v ? v : k;
-  const int64_t stride = is_q ? q_stride : is_v ? v_stride : k_stride;
-  h -= is_q ? 0 : is_v ? a.Hq + pg.Hkv : a.Hq;
-  if (is_q && a.q_out == nullptr) return;
-  int page = 0, slot = 0;
-  if (!is_q) {
-    slot = a.slots[t];
-    if (slot < 0) return;
-    page = slot >> pg.shift;
-    if (!pg.has(page)) return;
-  }
+  const int t = (int)(th / a.lanes);
   const int half = a.rot / 2;
-  const bool turns = !is_v && chunk * 16 < a.rot;
-  // the thread's two runs of 8 values
-  const int e0 = turns && !INTERLEAVED ? chunk * 8 : chunk * 16;
-  const int e1 = turns && !INTERLEAVED ? chunk * 8 + half : chunk * 16 + 8;
-  const In* src = reinterpret_cast<const In*>(in) + (int64_t)t * stride + (int64_t)h * pg.D;
-  float x[8], y[8];
-  load8(src + e0, x);
-  load8(src + e1, y);
-  if (turns) {
-    float c[8], s[8];  // of pairs [8 chunk, 8 chunk + 8)
+  const bool in_rot = chunk * 16 < a.rot;
+  float c[8], s[8];  // of pairs [8 chunk, 8 chunk + 8)
+  if (in_rot) {
+    const int pair = chunk * 8;
+    int axis[8];
+    bool one = true;  // axis for all of them
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int pair = chunk * 8 + i;
-      const int axis = a.pair_axis[pair];
-      const int pos = (uint32_t)axis < (uint32_t)a.n_axes ? a.positions[(int64_t)axis * a.T + t] : -1;
-      c[i] = s[i] = __builtin_nanf("");
-      if ((uint32_t)pos < (uint32_t)a.max_pos) {
-        c[i] = a.cos_table[(int64_t)pos * half + pair];
-        s[i] = a.sin_table[(int64_t)pos * half + pair];
-      }
+      axis[i] = a.pair_axis[pair + i];
+      one = one && axis[i] == axis[0];
     }
-    if constexpr (INTERLEAVED) {
+    const auto position = [&](int x) {
+      const int p = (uint32_t)x < (uint32_t)a.n_axes ? a.positions[(int64_t)x * a.T + t] : -1;
+      return (uint32_t)p < (uint32_t)a.max_pos ? p : -1;
+    };
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        turn(x[2 * i], x[2 * i + 1], c[i], s[i]);
-        turn(y[2 * i], y[2 * i + 1], c[4 + i], s[4 + i]);
+    for (int i = 0; i < 8; ++i) c[i] = s[i] = __builtin_nanf("");
+    if (one) {
+      const int p = position(axis[0]);
+      if (p >= 0) {
+        load8(a.cos_table + (int64_t)p * half + pair, c);
+        load8(a.sin_table + (int64_t)p * half + pair, s);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) turn(x[i], y[i], c[i], s[i]);
+      for (int i = 0; i < 8; ++i) {
+        const int p = position(axis[i]);
+        if (p >= 0) {
+          c[i] = a.cos_table[(int64_t)p * half + pair + i];
+          s[i] = a.sin_table[(int64_t)p * half + pair + i];
+        }
+      }
     }
   }
-  if (is_q) {
-    uint16_t* dst = a.q_out + ((int64_t)t * a.Hq + h) * pg.D;
-    store8_bf16(dst + e0, x);
-    store8_bf16(dst + e1, y);
-    return;
-  }
-  const int64_t row = pg.row(page, h, slot);
-  if constexpr (FP8) {
-    const float* scales = is_v ? v_scale : k_scale;
-    const float scale = scales ? scales[h] : 1.0f;
-    uint8_t* dst = reinterpret_cast<uint8_t*>(is_v ? v_cache : k_cache) + row;
-    store8_fp8(dst + e0, x, scale);
-    store8_fp8(dst + e1, y, scale);
-  } else {
-    uint16_t* dst = reinterpret_cast<uint16_t*>(is_v ? v_cache : k_cache) + row;
-    store8_bf16(dst + e0, x);
-    store8_bf16(dst + e1, y);
+  const int slot = a.slots[t];
+  const int page = slot >> pg.shift;
+  const bool stored = slot >= 0 && pg.has(page);
+  for (int head = (int)(th - (int64_t)t * a.lanes); head < a.heads; head += a.lanes) {
+    // heads: the queries', the keys', the values'
+    const bool is_q = head < a.Hq, is_v = head >= a.Hq + pg.Hkv;
+    if (is_q ? a.q_out == nullptr : !stored) continue;
+    const void* in = is_q ? q : is_v ? v : k;
+    const int64_t stride = is_q ? q_stride : is_v ? v_stride : k_stride;
+    const int h = head - (is_q ? 0 : is_v ? a.Hq + pg.Hkv : a.Hq);
+    const bool turns = !is_v && in_rot;
+    // the thread's two runs of 8 values
+    const int e0 = turns && !INTERLEAVED ? chunk * 8 : chunk * 16;
+    const int e1 = turns && !INTERLEAVED ? chunk * 8 + half : chunk * 16 + 8;
+    const In* src = reinterpret_cast<const In*>(in) + (int64_t)t * stride + (int64_t)h * pg.D;
+    float x[8], y[8];
+    load8(src + e0, x);
+    load8(src + e1, y);
+    if (turns) {
+      if constexpr (INTERLEAVED) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          turn(x[2 * i], x[2 * i + 1], c[i], s[i]);
+          turn(y[2 * i], y[2 * i + 1], c[4 + i], s[4 + i]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) turn(x[i], y[i], c[i], s[i]);
+      }
+    }
+    if (is_q) {
+      uint16_t* dst = a.q_out + ((int64_t)t * a.Hq + h) * pg.D;
+      store8_bf16(dst + e0, x);
+      store8_bf16(dst + e1, y);
+      continue;
+    }
+    const int64_t row = pg.row(page, h, slot);
+    if constexpr (FP8) {
+      const float* scales = is_v ? v_scale : k_scale;
+      const float scale = scales ? scales[h] : 1.0f;
+      uint8_t* dst = reinterpret_cast<uint8_t*>(is_v ? v_cache : k_cache) + row;
+      store8_fp8(dst + e0, x, scale);
+      store8_fp8(dst + e1, y, scale);
+    } else {
+      uint16_t* dst = reinterpret_cast<uint16_t*>(is_v ? v_cache : k_cache) + row;
+      store8_bf16(dst + e0, x);
+      store8_bf16(dst + e1, y);
+    }
   }
 }
 
@@ -184,7 +205,11 @@ extern "C" int moe_kv_append(const void* q, const void* k, const void* v, int64_
   a.T = T, a.n_axes = n_axes, a.max_pos = max_pos, a.rot = rot, a.Hq = d.Hq;
   a.heads = d.Hq + 2 * d.Hkv;
   a.chunk_shift = __builtin_ctz((unsigned)d.D) - 4;
-  a.threads = (int64_t)T * a.heads * (d.D / 16);
+  // as few threads a token as still fill the chip: 2048 for each CU
+  constexpr int64_t kFull = 256 * 2048;
+  a.lanes = a.heads;
+  while (a.lanes > 4 && (int64_t)T * ((a.lanes + 1) / 2) * (d.D / 16) >= kFull / 2) a.lanes = (a.lanes + 1) / 2;
+  a.threads = (int64_t)T * a.lanes * (d.D / 16);
   const int64_t blocks = (a.threads + eldr::kAppendThreads - 1) / eldr::kAppendThreads;
   if (blocks > 0x7fffffffLL) return MOE_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)blocks), block(eldr::kAppendThreads);
