@@ -26,7 +26,13 @@ namespace eldr {
 
 constexpr int kDecodeThreads = 256;
 constexpr int kDecodeWaves = kDecodeThreads / kWave;
-constexpr int kDecodeWgs = 768; // workgroups: three for each CU
+
+// Workgroups that share the own line.  More of them hide the ends of short
+// segments, fewer make longer segments and fewer parts.  Measured (us; 512, 768,
+// 1024): D = 128, 128 requests of up to 8000 178, 180, 182; 64 of up to 4000 51, 52,
+// 55; D = 64, 256 of up to 1500 in fp8 57, 50, 42.
+constexpr int decode_wgs(int D) { return D == 64 ? 1024 : 512; }
+
 
 struct DecodeArgs {
   const uint16_t* q;
@@ -52,7 +58,7 @@ struct Parts {
     own = ws;
     shared = own + rows * (D + 4);
     own_rest = shared + rows * (D + 4);
-    shared_rest = own_rest + (int64_t)kDecodeWgs * kRows * (D + 4);
+    shared_rest = own_rest + (int64_t)decode_wgs(D) * kRows * (D + 4);
     plan = reinterpret_cast<int*>(shared_rest + (int64_t)kSharedWgs * shared_rows * (D + 4));
   }
 };
@@ -103,8 +109,8 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, const Pages& pg, con
     const int64_t r0 = pg.row(has0 ? b0 : 0, sg.h, k) * T::kElem, r1 = pg.row(has1 ? b1 : 0, sg.h, k + 16) * T::kElem;
     Keys<D, FP8> k_lo, k_hi;
     Values<D, FP8> v;
-    k_lo.load(a.k_cache + r0, n, g);
-    k_hi.load(a.k_cache + r1, n, g);
+    k_lo.template load<true>(a.k_cache + r0, n, g);
+    k_hi.template load<true>(a.k_cache + r1, n, g);
     v.load(a.v_cache + r0, a.v_cache + r1, n, g);
     __builtin_amdgcn_sched_barrier(0);
     f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
@@ -205,7 +211,7 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void attn_decode_
     const int ints = 3 * R + 1 + n + 1;  // own, reach, group, shared
     for (int i = threadIdx.x; i < ints; i += kDecodeThreads) parts.plan[i] = plan.own[i];
   }
-  const Deal deal(row * pg.Hkv * a.head_tiles, kDecodeWgs);
+  const Deal deal(row * pg.Hkv * a.head_tiles, decode_wgs(D));
   if ((int)blockIdx.x >= deal.wgs) return;
   int u = __builtin_amdgcn_readfirstlane(deal.first(blockIdx.x));
   const int end = __builtin_amdgcn_readfirstlane(deal.first(blockIdx.x + 1));
@@ -264,7 +270,7 @@ __global__ __launch_bounds__(kDecodeThreads) void attn_join_kernel(DecodeArgs a,
     shared_at = row % kTileRows;
   }
   if (tiles > 0) {
-    const Deal deal(own_row * pg.Hkv * a.head_tiles, kDecodeWgs);
+    const Deal deal(own_row * pg.Hkv * a.head_tiles, decode_wgs(D));
     const int u0 = (h * a.head_tiles + i / kRows) * own_row + own[r];
     own_w0 = deal.owner(u0);
     own_parts = deal.owner(u0 + tiles - 1) - own_w0 + 1;
@@ -347,7 +353,7 @@ int launch_decode(const DecodeArgs& a, const Pages& pg, hipStream_t s) {
     if (!lds_allowed(reinterpret_cast<const void*>(attn_shared_kernel<D, FP8>), S::kBytes + plan)) return MOE_ERR_HIP;
     hipLaunchKernelGGL((attn_shared_kernel<D, FP8>), dim3(kSharedWgs), dim3(kSharedThreads), S::kBytes + plan, s, sh, pg);
   }
-  hipLaunchKernelGGL((attn_decode_kernel<D, FP8>), dim3(kDecodeWgs), dim3(kDecodeThreads), lds, s, a, pg, parts);
+  hipLaunchKernelGGL((attn_decode_kernel<D, FP8>), dim3(decode_wgs(D)), dim3(kDecodeThreads), lds, s, a, pg, parts);
   // measured (us): 64 rows of 192 parts 8 by 256 threads and 31 by 64; 16,384 rows of
   // about 10 parts 39 and 14
   constexpr int64_t kFewRows = 1024;

@@ -47,16 +47,24 @@ __device__ __forceinline__ StepPages step_pages(const Pages& pg, const int32_t* 
   return s;
 }
 
+// A load of what is read once (STREAM: it does not displace what the caches hold)
+// or again by other workgroups or the next call.
+template <bool STREAM, typename V>
+__device__ __forceinline__ V tile_load(const char* p) {
+  const V* v = reinterpret_cast<const V*>(p);
+  return STREAM ? __builtin_nontemporal_load(v) : *v;
+}
+
 // One 16-slot tile of keys as MFMA operands.
 template <int D, bool FP8>
 struct Keys {
   using T = Tile<D, FP8>;
   static constexpr int kLoads = FP8 ? T::kK / 2 : T::kK;
   u32x4 raw[kLoads];
+  template <bool STREAM>
   __device__ __forceinline__ void load(const char* rows, int n, int g) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-      raw[i] = *reinterpret_cast<const u32x4*>(rows + (uint32_t)(n * D * T::kElem + i * 64 + g * 16));
+    for (int i = 0; i < kLoads; ++i) raw[i] = tile_load<STREAM, u32x4>(rows + (uint32_t)(n * D * T::kElem + i * 64 + g * 16));
   }
   __device__ __forceinline__ u32x4 operand(int s) const {
     if constexpr (FP8) {
@@ -84,15 +92,15 @@ struct Values {
       if constexpr (kBytes >= 16) {
 #pragma unroll
         for (int w = 0; w < kWords; w += 4) {
-          const u32x4 x = *reinterpret_cast<const u32x4*>(p + 4 * w);
+          const u32x4 x = tile_load<true, u32x4>(p + 4 * w);
 #pragma unroll
           for (int i = 0; i < 4; ++i) raw[j][w + i] = x[i];
         }
       } else if constexpr (kBytes == 8) {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+        const u32x2 x = tile_load<true, u32x2>(p);
         raw[j][0] = x[0], raw[j][1] = x[1];
       } else {
-        raw[j][0] = *reinterpret_cast<const uint32_t*>(p);
+        raw[j][0] = tile_load<true, uint32_t>(p);
       }
     }
   }

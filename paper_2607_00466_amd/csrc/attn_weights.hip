@@ -123,8 +123,8 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
     s.pages = pages;
     pages = step_pages(pg, table, k + kStride);
     if (k >= sp.k1) return;
-    s.keys[0].load(a.k_cache + pg.row(pg.has(s.pages.b0) ? s.pages.b0 : 0, sp.h, k) * T::kElem, n, g);
-    s.keys[1].load(a.k_cache + pg.row(pg.has(s.pages.b1) ? s.pages.b1 : 0, sp.h, k + 16) * T::kElem, n, g);
+    s.keys[0].template load<false>(a.k_cache + pg.row(pg.has(s.pages.b0) ? s.pages.b0 : 0, sp.h, k) * T::kElem, n, g);
+    s.keys[1].template load<false>(a.k_cache + pg.row(pg.has(s.pages.b1) ? s.pages.b1 : 0, sp.h, k + 16) * T::kElem, n, g);
 #pragma unroll
     for (int t = 0; t < TILES; ++t)
 #pragma unroll
@@ -193,8 +193,8 @@ __device__ __forceinline__ void weigh_wide(const WeightArgs& a, const Pages& pg,
     const StepPages pages = step_pages(pg, table, k);
     const bool there[2] = {pg.has(pages.b0), pg.has(pages.b1)};
     Keys<D, FP8> keys[2];
-    keys[0].load(a.k_cache + pg.row(there[0] ? pages.b0 : 0, sp.h, k) * T::kElem, n, g);
-    keys[1].load(a.k_cache + pg.row(there[1] ? pages.b1 : 0, sp.h, k + 16) * T::kElem, n, g);
+    keys[0].template load<false>(a.k_cache + pg.row(there[0] ? pages.b0 : 0, sp.h, k) * T::kElem, n, g);
+    keys[1].template load<false>(a.k_cache + pg.row(there[1] ? pages.b1 : 0, sp.h, k + 16) * T::kElem, n, g);
     for (int row0 = sp.row0; row0 < sp.row1; row0 += a.pad) {
       const int r = sp.first + row0 / a.pad;
       if (r >= sp.end || (sp.group >= 0 && group[r] != sp.group)) continue;
