@@ -204,13 +204,10 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void attn_decode_
   __shared__ int waves[kDecodeWaves];
   float* sums_lds = reinterpret_cast<float*>(lds);
   int* plan_lds = lds + kDecodeWaves * kRows * (D + 4);
-  const int capacity = pg.capacity();
-  const Plan plan = make_plan<kDecodeThreads>(a.gr, capacity, a.G, SharedTile<D>::kRowsWg, plan_lds, waves);
+  const Plan plan = make_plan<kDecodeThreads>(a.gr, pg.capacity(), a.G, SharedTile<D>::kRowsWg, plan_lds, waves);
   const int R = a.gr.R, n = a.gr.n, row = plan.own[R];
-  if (blockIdx.x == 0) {
-    const int ints = 3 * R + 1 + n + 1;  // own, reach, group, shared
-    for (int i = threadIdx.x; i < ints; i += kDecodeThreads) parts.plan[i] = plan.own[i];
-  }
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < Plan::kept(R, n); i += kDecodeThreads) parts.plan[i] = plan.own[i];
   const Deal deal(row * pg.Hkv * a.head_tiles, decode_wgs(D));
   if ((int)blockIdx.x >= deal.wgs) return;
   int u = __builtin_amdgcn_readfirstlane(deal.first(blockIdx.x));
@@ -220,7 +217,7 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void attn_decode_
   while (u < end) {
     const int hv = u / row, v = u - hv * row;
     const int r = last_at(plan.own, R, v), t = v - plan.own[r];
-    const int len = clamp_len(a.gr.lens[r], capacity), reach = plan.reach[r];
+    const int len = plan.len[r], reach = plan.reach[r];
     const int lo = own_from(len, reach, a.gr.window), t0 = lo / kTile;
     const int tiles = __builtin_amdgcn_readfirstlane(min(plan.own[r + 1] - v, end - u));
     const bool begins = t == 0, whole = begins && v + tiles == plan.own[r + 1] && reach == 0;

@@ -17,7 +17,7 @@
 
 namespace eldr {
 
-constexpr int kTile = 128;  // slots of a unit; tiles start at multiples of it
+constexpr int kTile = 128;  // slots of a unit; units start at multiples of it
 
 struct Groups {
   const int32_t *lens, *start, *prefix;
@@ -26,13 +26,17 @@ struct Groups {
 
 // The plan in LDS.
 struct Plan {
-  int *own;     // [R + 1] own tiles before each request
+  int *own;     // [R + 1] own units before each request
   int *reach;   // [R] slots read with the group
   int *group;   // [R] the request's group, -1: none
   int *shared;  // [n + 1] shared units (row tiles x slot tiles) before each group
   int *least;   // [n] slots the group shares
+  int *len;     // [R] cached slots
+  int *start;   // [n + 1] the groups' first requests
 
-  static __host__ __device__ size_t bytes(int R, int n) { return sizeof(int) * (3 * (size_t)R + 1 + 2 * (size_t)n + 1); }
+  // own, reach, group and shared: what moe_attn_decode leaves for its join
+  static __host__ __device__ int kept(int R, int n) { return 3 * R + 1 + n + 1; }
+  static __host__ __device__ size_t bytes(int R, int n) { return sizeof(int) * ((size_t)kept(R, n) + n + R + n + 1); }
 };
 
 // out[0] = 0, out[i + 1] = sum of f(0 .. i), by THREADS threads, i ascending a thread.
@@ -56,6 +60,7 @@ __device__ __forceinline__ void sums(int n, int* out, int* waves, F f) {
   __syncthreads();
 }
 
+// Tiles that [lo, hi) touches.
 __device__ __forceinline__ int tiles_of(int lo, int hi) {
   return hi > lo ? (hi + kTile - 1) / kTile - lo / kTile : 0;
 }
@@ -68,7 +73,8 @@ __device__ __forceinline__ int own_from(int n, int reach, int window) {
 }
 
 // Works the plan out.  `lds`: Plan::bytes of LDS; `waves`: THREADS / 64 ints of
-// LDS; G: query heads a kv head; row_tile: rows of a shared unit.
+// LDS; G: query heads a kv head; row_tile: rows of a shared unit.  What is read
+// from memory is asked for at once, and the rest is LDS.
 template <int THREADS>
 __device__ __forceinline__ Plan make_plan(const Groups& gr, int capacity, int G, int row_tile, int* lds, int* waves) {
   Plan p;
@@ -77,42 +83,43 @@ __device__ __forceinline__ Plan make_plan(const Groups& gr, int capacity, int G,
   p.group = p.reach + gr.R;
   p.shared = p.group + gr.R;
   p.least = p.shared + gr.n + 1;
-  int* least = p.least;
-  for (int g = threadIdx.x; g < gr.n; g += THREADS) least[g] = clamp_len(gr.prefix[g], capacity);
+  p.len = p.least + gr.n;
+  p.start = p.len + gr.R;
+  for (int r = threadIdx.x; r < gr.R; r += THREADS) p.len[r] = clamp_len(gr.lens[r], capacity);
+  for (int g = threadIdx.x; g < gr.n; g += THREADS) {
+    p.least[g] = clamp_len(gr.prefix[g], capacity);
+    p.start[g] = min(max(gr.start[g], 0), gr.R);
+  }
+  if (gr.n > 0 && threadIdx.x == 0) p.start[gr.n] = min(max(gr.start[gr.n], 0), gr.R);
   __syncthreads();
   for (int r = threadIdx.x; r < gr.R; r += THREADS) {
     int group = -1;
     if (gr.n > 0) {
-      // the last group that starts at or before r
-      int lo = 0, hi = gr.n;  // starts[lo] <= r is not known for lo = 0
+      // the last group that starts at or before r (the first one may not)
+      int lo = 0, hi = gr.n;
       while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
-        if (gr.start[mid] <= r) lo = mid;
+        if (p.start[mid] <= r) lo = mid;
         else hi = mid;
       }
-      const int s = max(gr.start[lo], 0), e = min(gr.start[lo + 1], gr.R);
-      if (s <= r && r < e && e - s > 1) {
-        // an empty member reads nothing and does not shorten what the others share
-        const int n = clamp_len(gr.lens[r], capacity);
-        if (n > 0) {
-          group = lo;
-          atomicMin(&least[lo], n);
-        }
+      const int s = p.start[lo], e = p.start[lo + 1];
+      // an empty member reads nothing and does not shorten what the others share
+      if (s <= r && r < e && e - s > 1 && p.len[r] > 0) {
+        group = lo;
+        atomicMin(&p.least[lo], p.len[r]);
       }
     }
     p.group[r] = group;
   }
   __syncthreads();
-  for (int r = threadIdx.x; r < gr.R; r += THREADS) p.reach[r] = p.group[r] < 0 ? 0 : least[p.group[r]];
+  for (int r = threadIdx.x; r < gr.R; r += THREADS) p.reach[r] = p.group[r] < 0 ? 0 : p.least[p.group[r]];
   __syncthreads();
-  sums<THREADS>(gr.R, p.own, waves, [&](int r) {
-    const int n = clamp_len(gr.lens[r], capacity);
-    return tiles_of(own_from(n, p.reach[r], gr.window), n);
-  });
+  sums<THREADS>(gr.R, p.own, waves,
+                [&](int r) { return tiles_of(own_from(p.len[r], p.reach[r], gr.window), p.len[r]); });
   if (gr.n > 0)
     sums<THREADS>(gr.n, p.shared, waves, [&](int g) {
-      const int s = max(gr.start[g], 0), e = min(gr.start[g + 1], gr.R);
-      return e - s > 1 ? ((e - s) * G + row_tile - 1) / row_tile * tiles_of(0, least[g]) : 0;
+      const int members = p.start[g + 1] - p.start[g];
+      return members > 1 ? (members * G + row_tile - 1) / row_tile * tiles_of(0, p.least[g]) : 0;
     });
   else if (threadIdx.x == 0)
     p.shared[0] = 0;

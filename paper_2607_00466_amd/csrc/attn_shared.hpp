@@ -307,7 +307,7 @@ __global__ __launch_bounds__(kSharedThreads, 2) void attn_shared_kernel(SharedAr
   __shared__ int waves[kSharedWaves];
   const int capacity = pg.capacity();
   const Plan plan = make_plan<kSharedThreads>(a.gr, capacity, a.G, S::kRowsWg, reinterpret_cast<int*>(lds_shared + S::kBytes), waves);
-  const int R = a.gr.R, n = a.gr.n, row = plan.shared[n];
+  const int n = a.gr.n, row = plan.shared[n];
   const Deal deal(row * pg.Hkv, kSharedWgs);
   const int w = (int)blockIdx.x % kNumXcd * (kSharedWgs / kNumXcd) + (int)blockIdx.x / kNumXcd;
   if (w >= deal.wgs) return;
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(kSharedThreads, 2) void attn_shared_kernel(SharedAr
   while (u < end) {
     const int h = u / row, v = u - h * row;
     const int grp = last_at(plan.shared, n, v);
-    const int first = max(a.gr.start[grp], 0), members = min(a.gr.start[grp + 1], R) - first;
+    const int first = plan.start[grp], members = plan.start[grp + 1] - first;
     const int reach = plan.least[grp], per = tiles_of(0, reach), in = v - plan.shared[grp];
     const int tile = in / per, t = in - tile * per;
     const int tiles = __builtin_amdgcn_readfirstlane(min(per - t, end - u));

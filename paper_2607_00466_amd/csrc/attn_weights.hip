@@ -245,7 +245,7 @@ __global__ __launch_bounds__(kWeightThreads, 2) void attn_weights_kernel(WeightA
     if (u < shared_units) {
       const int h = u / shared_row, v = u - h * shared_row;
       const int grp = last_at(plan.shared, n, v);
-      const int first = max(a.gr.start[grp], 0), last = min(a.gr.start[grp + 1], R), reach = plan.least[grp];
+      const int first = plan.start[grp], last = plan.start[grp + 1], reach = plan.least[grp];
       const int per = tiles_of(0, reach), in = v - plan.shared[grp], run = in / per, t = in - run * per;
       tiles = min(per - t, end - u);
       sp = Span{first, first, last, grp, run * member_rows, min((run + 1) * member_rows, (last - first) * a.pad), h,
@@ -253,7 +253,7 @@ __global__ __launch_bounds__(kWeightThreads, 2) void attn_weights_kernel(WeightA
     } else {
       const int o = u - shared_units, h = o / own_row, v = o - h * own_row;
       const int r = last_at(plan.own, R, v), t = v - plan.own[r];
-      const int len = clamp_len(a.gr.lens[r], capacity), lo = min(plan.reach[r], len), t0 = lo / kTile;
+      const int len = plan.len[r], lo = min(plan.reach[r], len), t0 = lo / kTile;
       tiles = min(plan.own[r + 1] - v, end - u);
       sp = Span{r, r, r + 1, -1, 0, a.pad, h, max((t0 + t) * kTile, lo), min((t0 + t + tiles) * kTile, len)};
     }
