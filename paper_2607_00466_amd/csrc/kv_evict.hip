@@ -399,12 +399,13 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_long_kernel(EvictArg
   }
 }
 
-// One workgroup a (request, kv head, run of kMoveSlots slots): the moved ones
-// are listed in LDS, then 16 bytes a thread, a row's pieces on neighbouring
-// lanes, keys and values in turn.
-__global__ __launch_bounds__(kMoveThreads) void kv_move_kernel(EvictArgs a, Pages pg, void* k_cache, void* v_cache,
-                                                               int row_shift, int elem) {
-  __shared__ int to[kMoveSlots], from[kMoveSlots], count;
+// One workgroup a (request, kv head, run of kMoveSlots slots): the moved rows'
+// offsets are listed in LDS, pages looked up once a row, then 16 bytes a thread
+// and four of them in flight, a row's pieces on neighbouring lanes.
+__global__ __launch_bounds__(kMoveThreads) void kv_move_kernel(EvictArgs a, Pages pg, char* k_cache, char* v_cache, int row_shift,
+                                                               int elem) {
+  __shared__ int64_t to[kMoveSlots], from[kMoveSlots];  // bytes
+  __shared__ int count;
   const int rh = blockIdx.y, r = rh / pg.Hkv, h = rh % pg.Hkv;
   if (min(max(a.lens[r], 0), a.N) <= a.budget) return;
   if (threadIdx.x == 0) count = 0;
@@ -413,16 +414,34 @@ __global__ __launch_bounds__(kMoveThreads) void kv_move_kernel(EvictArgs a, Page
   if (i < a.budget) {
     const int s = a.src[(int64_t)rh * a.budget + i];
     if (s != i) {
-      const int at = atomicAdd(&count, 1);  // any order: the rows are copied independently
-      to[at] = i;
-      from[at] = s;
+      const int bt = pg.page(r, i), bf = pg.page(r, s);
+      if (pg.has(bt) && pg.has(bf)) {
+        const int at = atomicAdd(&count, 1);  // any order: the rows are copied independently
+        to[at] = pg.row(bt, h, i) * elem;
+        from[at] = pg.row(bf, h, s) * elem;
+      }
     }
   }
   __syncthreads();
-  const int pieces = 2 << row_shift;  // of 16 bytes, of a slot's keys and values
-  for (int p = threadIdx.x; p < count * pieces; p += kMoveThreads) {
-    const int m = p / pieces;
-    copy_piece(pg, k_cache, v_cache, r, h, to[m], from[m], p - m * pieces, row_shift, elem);
+  const int pieces = count << row_shift;  // of one cache
+  constexpr int kBatch = 4;
+#pragma unroll
+  for (int v = 0; v < 2; ++v) {
+    char* cache = v ? v_cache : k_cache;
+    for (int p0 = threadIdx.x; p0 < pieces; p0 += kBatch * kMoveThreads) {
+      u32x4 x[kBatch];
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        const int p = min(p0 + b * kMoveThreads, pieces - 1);
+        x[b] = __builtin_nontemporal_load(
+            reinterpret_cast<const u32x4*>(cache + from[p >> row_shift] + (p & ((1 << row_shift) - 1)) * 16));
+      }
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        const int p = p0 + b * kMoveThreads;
+        if (p < pieces) *reinterpret_cast<u32x4*>(cache + to[p >> row_shift] + (p & ((1 << row_shift) - 1)) * 16) = x[b];
+      }
+    }
   }
 }
 
@@ -489,6 +508,7 @@ extern "C" int moe_kv_evict(const float* weights, const int32_t* pos, const int3
   st = launch_status();
   if (st != MOE_OK || a.N <= budget || (moves && a.N <= eldr::kShortRow)) return st;
   const dim3 grid((budget + eldr::kMoveSlots - 1) / eldr::kMoveSlots, d.R * d.Hkv);
-  hipLaunchKernelGGL(eldr::kv_move_kernel, grid, dim3(eldr::kMoveThreads), 0, s, a, pg, k_cache, v_cache, row_shift, elem);
+  hipLaunchKernelGGL(eldr::kv_move_kernel, grid, dim3(eldr::kMoveThreads), 0, s, a, pg, static_cast<char*>(k_cache),
+                     static_cast<char*>(v_cache), row_shift, elem);
   return launch_status();
 }
