@@ -68,16 +68,15 @@ __device__ __forceinline__ void add_weights(const f32x4& s, float unit, const f3
 // The sums over the `in_tile` rows of each request of a 16-row tile: in element
 // c of the lanes whose row 4 (lane / 16) + c is a request's first.
 __device__ __forceinline__ void sum_heads(f32x4& x, int in_tile) {
-  if (in_tile >= 2) x[0] += x[1], x[2] += x[3];
-  if (in_tile >= 4) x[0] += x[2];
-  if (in_tile >= 8) {
-    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[0]), __float_as_uint(x[0]), false, false);
-    x[0] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-  }
-  if (in_tile >= 16) {
-    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[0]), __float_as_uint(x[0]), false, false);
-    x[0] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-  }
+  // (selects, not branches: a branch would keep the row tiles from overlapping)
+  const float two = x[2] + x[3];
+  x[0] += in_tile >= 2 ? x[1] : 0.0f;
+  x[2] = in_tile >= 2 ? two : x[2];
+  x[0] += in_tile >= 4 ? x[2] : 0.0f;
+  const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[0]), __float_as_uint(x[0]), false, false);
+  x[0] = in_tile >= 8 ? __uint_as_float(p[0]) + __uint_as_float(p[1]) : x[0];
+  const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[0]), __float_as_uint(x[0]), false, false);
+  x[0] = in_tile >= 16 ? __uint_as_float(q[0]) + __uint_as_float(q[1]) : x[0];
 }
 
 // The tiles of rows from sp.row0 on, of requests of up to 16 rows; a lane has up
@@ -95,13 +94,16 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
   u32x4 q[TILES][T::kK];
   f32x4 lse[TILES];
   int64_t at[TILES];    // of the lane's first request's weights, at slot 0
+  int past[TILES];      // requests of the span after that one
   uint32_t mine = 0;    // bit PER t + c: the lane writes its c-th request of tile t
 #pragma unroll
   for (int t = 0; t < TILES; ++t) {
     const int row0 = sp.row0 + t * kRows;
     load_rows<D, FP8>(a, sp, row0, q[t], lse[t]);
-    const int first = sp.first + (row0 + 4 * g) / a.pad;
+    // (kept within the span's requests, so that what it names can always be read)
+    const int first = min(sp.first + (row0 + 4 * g) / a.pad, sp.end - 1);
     at[t] = ((int64_t)first * pg.Hkv + sp.h) * N;
+    past[t] = sp.end - 1 - first;
 #pragma unroll
     for (int c = 0; c < PER; ++c) {
       const int row = row0 + 4 * g + c * kEach, r = sp.first + row / a.pad;
@@ -125,18 +127,16 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
     if (k >= sp.k1) return;
     s.keys[0].template load<false>(a.k_cache + pg.row(pg.has(s.pages.b0) ? s.pages.b0 : 0, sp.h, k) * T::kElem, n, g);
     s.keys[1].template load<false>(a.k_cache + pg.row(pg.has(s.pages.b1) ? s.pages.b1 : 0, sp.h, k + 16) * T::kElem, n, g);
+    if (a.weights_in) {
+      // every lane reads something of the span's rows, so that no load is behind a branch
+      const int slots[2] = {k + n, min(k + 16 + n, (int)N - 1)};
 #pragma unroll
-    for (int t = 0; t < TILES; ++t)
+      for (int t = 0; t < TILES; ++t)
 #pragma unroll
-      for (int c = 0; c < PER; ++c) {
-        const float* from = a.weights_in + at[t] + c * next_request + k + n;
+        for (int c = 0; c < PER; ++c)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          float x = 0.0f;
-          if (a.weights_in && (mine >> (PER * t + c) & 1u) && counts(k + 16 * b + n)) x = from[16 * b];
-          s.before[t][b][c] = x;
-        }
-      }
+          for (int b = 0; b < 2; ++b) s.before[t][b][c] = a.weights_in[at[t] + min(c, past[t]) * next_request + slots[b]];
+    }
   };
   const auto use = [&](Set& st, int k) {
     float sum[TILES][2][PER];
@@ -158,14 +158,29 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
       }
     }
     const bool there[2] = {pg.has(st.pages.b0), pg.has(st.pages.b1)};
+    const auto put = [&](int t, int b, int c) {
+      a.weights_out[at[t] + c * next_request + k + n + 16 * b] =
+          (a.weights_in ? st.before[t][b][c] : 0.0f) + (there[b] ? sum[t][b][c] : 0.0f);
+    };
+    constexpr uint32_t kAll = TILES * PER < 32 ? (1u << (TILES * PER)) - 1 : ~0u;
+    if (k >= sp.k0 && k + kStep <= sp.k1 && __all(mine == 0 || mine == kAll)) {
+      if (mine == kAll) {
 #pragma unroll
-    for (int t = 0; t < TILES; ++t)
+        for (int t = 0; t < TILES; ++t)
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+          for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int c = 0; c < PER; ++c)
-          if ((mine >> (PER * t + c) & 1u) && counts(k + 16 * b + n))
-            a.weights_out[at[t] + c * next_request + k + n + 16 * b] = st.before[t][b][c] + (there[b] ? sum[t][b][c] : 0.0f);
+            for (int c = 0; c < PER; ++c) put(t, b, c);
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int c = 0; c < PER; ++c)
+            if ((mine >> (PER * t + c) & 1u) && counts(k + 16 * b + n)) put(t, b, c);
+    }
   };
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) fetch(sets[i], k_first + i * kStride);
@@ -236,9 +251,10 @@ __global__ __launch_bounds__(kWeightThreads, 2) void attn_weights_kernel(WeightA
   // one line: the shared units, then the own ones
   const int shared_units = shared_row * pg.Hkv;
   const Deal deal(shared_units + own_row * pg.Hkv, wgs);
-  if ((int)blockIdx.x >= deal.wgs) return;
-  int u = __builtin_amdgcn_readfirstlane(deal.first(blockIdx.x));
-  const int end = __builtin_amdgcn_readfirstlane(deal.first(blockIdx.x + 1));
+  const int w = blockIdx.x;
+  if (w >= deal.wgs) return;
+  int u = __builtin_amdgcn_readfirstlane(deal.first(w));
+  const int end = __builtin_amdgcn_readfirstlane(deal.first(w + 1));
   while (u < end) {
     Span sp;
     int tiles;
