@@ -700,11 +700,12 @@ def attn_dims(R: int, Hq: int, Hkv: int, D: int, block_size: int, max_blocks: in
 
 
 def _need_cache(t: torch.Tensor, name: str, d: AttnDims) -> None:
-    dense = d.Hkv * d.block_size * d.D
+    Hkv, bs, D = d.Hkv, d.block_size, d.D
+    dense = Hkv * bs * D
     if (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is _KV_DTYPES[d.kv_type]
-            and t.shape == (d.num_blocks, d.Hkv, d.block_size, d.D)
+            and t.shape == (d.num_blocks, Hkv, bs, D)
             and (t.is_contiguous() if d.block_stride in (0, dense)
-                 else t.stride() == (d.block_stride, d.block_size * d.D, d.D, 1) or t.numel() == 0)):
+                 else t.stride() == (d.block_stride, bs * D, D, 1) or t.numel() == 0)):
         return
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a torch tensor")
@@ -723,6 +724,10 @@ def _need_opt(t, name: str, dtype: torch.dtype, numel: int) -> None:
 
 def _need_rows(t: torch.Tensor, name: str, T: int, heads: int, D: int) -> int:
     """A [T, heads, D] tensor whose heads and values are contiguous; its token stride."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.shape == (T, heads, D):
+        token, head, value = t.stride()
+        if value == 1 and head == D and T > 1:
+            return token
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a torch tensor")
     if t.device.type != "cuda":
@@ -751,7 +756,7 @@ def moe_kv_append(q, k, v, positions, pair_axis, cos, sin, slots, d: AttnDims, q
     """Rotate q [T, Hq, D] into q_out and k [T, Hkv, D] by positions [n_axes, T], and
     store k and v in the caches' slots.  q, k and v may be views of one projection's
     rows; q and q_out may be None where only keys and values are wanted."""
-    T = slots.numel()
+    T, Hq, Hkv, D = slots.numel(), d.Hq, d.Hkv, d.D
     if positions.dim() != 2 or positions.shape[1] != T:
         raise ValueError(f"positions: expected [n_axes, {T}]")
     if cos.dim() != 2 or cos.shape != sin.shape:
@@ -761,26 +766,33 @@ def moe_kv_append(q, k, v, positions, pair_axis, cos, sin, slots, d: AttnDims, q
     n_axes, (max_pos, half) = positions.shape[0], cos.shape
     if pair_axis.numel() != half:
         raise ValueError(f"pair_axis: expected {half} axes, one a pair")
-    q_stride = 0
-    if q is not None:
-        q_stride = _need_rows(q, "q", T, d.Hq, d.D)
-        _need(q_out, "q_out", torch.bfloat16, T * d.Hq * d.D)
-    k_stride, v_stride = _need_rows(k, "k", T, d.Hkv, d.D), _need_rows(v, "v", T, d.Hkv, d.D)
-    if k.dtype not in _IN_TYPES or v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
+    dtype = k.dtype
+    if dtype not in _IN_TYPES or v.dtype is not dtype or (q is not None and q.dtype is not dtype):
         raise ValueError("q, k and v: expected all torch.bfloat16 or all torch.float32")
-    _need(positions, "positions", torch.int32, n_axes * T)
-    _need(pair_axis, "pair_axis", torch.int32, half)
-    _need(cos, "cos", torch.float32, max_pos * half)
-    _need(sin, "sin", torch.float32, max_pos * half)
-    _need(slots, "slots", torch.int32, T)
-    _need_opt(k_scale, "k_scale", torch.float32, d.Hkv)
-    _need_opt(v_scale, "v_scale", torch.float32, d.Hkv)
+    q_stride = pq = pq_out = 0
+    if q is not None:
+        q_stride = _need_rows(q, "q", T, Hq, D)
+        _need(q_out, "q_out", torch.bfloat16, T * Hq * D)
+        pq, pq_out = q.data_ptr(), q_out.data_ptr()
+    k_stride, v_stride = _need_rows(k, "k", T, Hkv, D), _need_rows(v, "v", T, Hkv, D)
+    i32, f32 = torch.int32, torch.float32
+    _need(positions, "positions", i32, n_axes * T)
+    _need(pair_axis, "pair_axis", i32, half)
+    _need(cos, "cos", f32, max_pos * half)
+    _need(sin, "sin", f32, max_pos * half)
+    _need(slots, "slots", i32, T)
+    if k_scale is not None:
+        _need(k_scale, "k_scale", f32, Hkv)
+    if v_scale is not None:
+        _need(v_scale, "v_scale", f32, Hkv)
     _need_cache(k_cache, "k_cache", d)
     _need_cache(v_cache, "v_cache", d)
-    _check("moe_kv_append", load().moe_kv_append(
-        _ptr(q), _ptr(k), _ptr(v), q_stride, k_stride, v_stride, _IN_TYPES[k.dtype], T, _ptr(positions), n_axes,
-        _ptr(pair_axis), _ptr(cos), _ptr(sin), max_pos, 2 * half, int(bool(interleaved)), _ptr(slots), d,
-        _ptr(k_scale), _ptr(v_scale), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _stream(stream)))
+    status = load().moe_kv_append(
+        pq, k.data_ptr(), v.data_ptr(), q_stride, k_stride, v_stride, _IN_TYPES[dtype], T, positions.data_ptr(), n_axes,
+        pair_axis.data_ptr(), cos.data_ptr(), sin.data_ptr(), max_pos, 2 * half, 1 if interleaved else 0, slots.data_ptr(), d,
+        _ptr(k_scale), _ptr(v_scale), pq_out, k_cache.data_ptr(), v_cache.data_ptr(), _stream(stream))
+    if status:
+        _check("moe_kv_append", status)
 
 
 def moe_attn_workspace_bytes(d: AttnDims) -> int:

@@ -73,7 +73,8 @@ def _run(cmd: list[str]) -> None:
     # (the remarks' source excerpts and carets are dropped with them)
     err = "\n".join(l for l in err.splitlines() if l.strip() and not l.lstrip().startswith(("|", "^")) and
                     not re.match(r"\s*\d+ \|", l))
-    if err.strip():
+    # nor is a remark's include path, where nothing else was said
+    if any(not l.startswith("In file included from") for l in err.splitlines()):
         print(err, file=sys.stderr)
 
 
