@@ -84,6 +84,39 @@ def test_append(T, Hq, Hkv, D, rot, axes, interleaved, fp8, dtype, bs, fused):
         assert torch.equal(got.float().cpu(), want)
 
 
+@pytest.mark.parametrize("T,axes,interleaved,fp8", [(3001, 1, False, False), (2049, 3, True, True)])
+def test_append_prompts(T, axes, interleaved, fp8):
+    # tokens enough for a thread to turn several heads
+    G.say(f"case: append of a prompt of {T}, {axes} axes, interleaved={interleaved} fp8={fp8}")
+    Hq, Hkv, D, rot, bs = 33, 3, 128, 96, 16
+    g = torch.Generator(device="cuda").manual_seed(T)
+    rows = torch.randn((T, Hq + 2 * Hkv, D), device="cuda", generator=g)
+    cos, sin = (x.cuda() for x in _tables(rot, 5000))
+    pos = torch.randint(0, 5000, (axes, T), device="cuda", generator=g, dtype=torch.int32)
+    axis = (torch.arange(rot // 2, device="cuda") * axes // (rot // 2)).to(torch.int32)  # its sections end inside a chunk
+    nb = -(-T // bs) + 1
+    slots = torch.randperm(nb * bs, device="cuda", generator=g)[:T].to(torch.int32)
+    dtype = U.FP8 if fp8 else torch.bfloat16
+    caches = [torch.zeros((nb, Hkv, bs, D), device="cuda").to(dtype) for _ in "kv"]
+    scale = torch.linspace(0.01, 2, Hkv, device="cuda") if fp8 else None
+    q_out = torch.empty((T, Hq, D), dtype=torch.bfloat16, device="cuda")
+    B.moe_kv_append(rows[:, :Hq], rows[:, Hq:-Hkv], rows[:, -Hkv:], pos, axis, cos, sin, slots,
+                    B.attn_dims(0, Hq, Hkv, D, bs, 1, nb, dtype), q_out, *caches, scale, scale, interleaved=interleaved)
+    at = pos.long()[axis.long()].T
+    i = torch.arange(rot // 2, device="cuda")
+    c, s = cos[at, i][:, None], sin[at, i][:, None]
+    lo, hi = (2 * i, 2 * i + 1) if interleaved else (i, i + rot // 2)
+    turned = rows[:, :-Hkv].clone()
+    a, b = turned[..., lo], turned[..., hi]
+    ac, bs_, bc, as_ = a * c, b * s, b * c, a * s
+    turned[..., lo], turned[..., hi] = ac - bs_, bc + as_
+    assert torch.equal(q_out, turned[:, :Hq].bfloat16())
+    for cache, x in zip(caches, (turned[:, Hq:], rows[:, -Hkv:])):
+        want = (x / scale[:, None]).clamp(-448, 448).to(dtype) if fp8 else x.to(dtype)
+        got = cache.float()[slots.long() // bs, :, slots.long() % bs]
+        assert torch.equal(got, want.float())
+
+
 def test_append_positions_outside_and_keys_alone():
     G.say("case: append, positions outside the table; keys and values alone; T = 0")
     cos, sin = (t.cuda() for t in _tables(64))
@@ -136,6 +169,10 @@ DECODE = [
     ([600, 640, 800], 5, 1, 128, 16, ((0, 2, 592),), False, 0, False),
     ([90, 95, 99], 8, 2, 64, 16, ((0, 3, 64),), False, 20, False),  # a window: nothing is shared
     ([1100 + i for i in range(70)], 32, 4, 128, 16, ((0, 70, 1088),), False, 0, False),
+    # prefixes of several look-up windows, rows that leave row waves idle
+    ([2600, 2501, 2550, 2500], 20, 4, 64, 64, ((0, 4, 2500),), True, 0, True),
+    ([3100, 3201, 3150], 16, 2, 256, 16, ((0, 3, 3100),), False, 0, False),
+    ([2100] * 5, 48, 1, 128, 16, ((0, 5, 2048),), False, 0, False),
 ]
 
 
@@ -164,6 +201,21 @@ def test_decode_large_batch_of_many_groups(fp8):
     # a page that a short member reads through the first one has to be there
     cache = U.Cache(lens, 2, 64, 16, fp8, seed=9, shared=shared)
     U.run_decode(cache, U.queries(300, 8, 64), shared)
+
+
+@pytest.mark.parametrize("D,fp8", [(64, True), (256, False)])
+def test_decode_most_requests_and_groups(D, fp8):
+    G.say(f"case: decode of 1024 requests in 512 groups of two, D={D}: the largest plan")
+    rng = np.random.default_rng(D)
+    lens = [int(x) for x in rng.integers(0, 70, 1024)]
+    shared = []
+    for s in range(0, 1024, 2):
+        n = 16 * int(rng.integers(0, 3))
+        shared.append((s, s + 2, n))
+        lens[s] += n
+        lens[s + 1] += n
+    cache = U.Cache(lens, 1, D, 16, fp8, seed=D, shared=shared)
+    U.run_decode(cache, U.queries(1024, 2, D), shared)
 
 
 def test_decode_peaked_and_flat_scores():
@@ -312,6 +364,10 @@ EVICT = [
     ([513, 640], 2, 128, 16, 511, 0, None, False, "zero"),
     ([20000], 1, 64, 16, 9000, 100, [3], False, "ties"),
     ([70000], 1, 64, 16, 12345, 100, [3], True, "random"),
+    ([500, 480, 512], 2, 64, 16, 448, 5, None, False, "ties"),   # one wave a row, its few moves in the same launch
+    ([8192, 8140], 1, 128, 16, 8128, 0, [2, 2], True, "zero"),   # 64 moves at most
+    ([8193, 8000], 1, 64, 16, 4096, 9, None, False, "odd"),      # the longest rows that eight keys a lane hold, and over
+    ([32768, 20000], 1, 64, 16, 16384, 0, None, False, "random"),
 ]
 
 
