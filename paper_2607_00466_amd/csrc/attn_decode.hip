@@ -2,10 +2,10 @@
 //
 // One pass over the keys and values with the running maximum and sum of the
 // softmax.  A wave takes 32 slots at a time for 16 query rows (the query heads
-// of one kv head; of several requests where a prefix is shared):
+// of one kv head):
 //
 //   S^T = K Q^T   two 16x16 tiles of (slot, row), MFMA over D
-//   P   = exp2(S^T - max), in the lanes that the products left it in
+//   P   = exp2(S^T - m), in the lanes that the products left it in
 //   O^T += V^T P  MFMA over the 32 slots
 //
 // The reduction over slots may take them in any order that both operands share,
@@ -13,7 +13,12 @@
 // holds P already: no shuffle and no LDS between the two products.  Keys and
 // values go from HBM to registers directly: a lane loads 16 bytes of one row,
 // and a value tile is transposed inside the lane (its rows' 16-bit halves are
-// zipped by v_perm).  What bounds it is HBM: 64 KB of rows a unit.
+// zipped by v_perm).  What bounds it is HBM, by loads that do not displace what
+// the caches hold (non-temporal; 203 -> 178 us in the first case below).  Measured:
+// 128 requests of up to 8000 tokens (32 heads over 4 of 128, bf16) 175 us, 6.3 TB/s
+// of a streaming read's 7.05; 64 x 16384 in fp8 174 us; D = 64 339 us and D = 256
+// 355 us for 2.1 GB.  Dealing the units to waves in place of workgroups (no merge in
+// LDS, four times the parts) measured 2 to 8% slower.
 //
 // The four waves of a workgroup take turns at a segment's 32-slot steps and
 // meet in LDS at its end.  A segment that is a request's whole context gives
@@ -33,7 +38,6 @@ constexpr int kDecodeWaves = kDecodeThreads / kWave;
 // 55; D = 64, 256 of up to 1500 in fp8 57, 50, 42.
 constexpr int decode_wgs(int D) { return D == 64 ? 1024 : 512; }
 
-
 struct DecodeArgs {
   const uint16_t* q;
   const char *k_cache, *v_cache;
@@ -41,7 +45,6 @@ struct DecodeArgs {
   const float *k_scale, *v_scale, *sinks;
   uint16_t* out;
   float* lse;
-  float* ws;
   float scale;
   int32_t Hq, G, head_tiles;  // head_tiles: ceil(G / kRows)
 };
@@ -63,13 +66,10 @@ struct Parts {
   }
 };
 
-// A run of slots [k0, k1) of a request's (or group's) context against up to
-// kRows query rows.
+// A run of slots [k0, k1) of a request against a tile of its heads: rows
+// [row0, row0 + kRows) of the G heads of kv head h.
 struct Segment {
-  int table_row;        // request whose block table names the pages
-  int first, rows;      // requests from `first` on, rows of kv head h: row i is head h G + i % G of request first + i / G
-  int row0;             // first row of the tile
-  int h, k0, k1;
+  int request, row0, h, k0, k1;
 };
 
 // The running state of 16 rows: maximum and sum (this lane's part) of row
@@ -87,9 +87,8 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, const Pages& pg, con
   u32x4 q[T::kK];
   {
     const int row = sg.row0 + n;
-    const bool live = row < sg.rows;
-    const int req = sg.first + (live ? row / a.G : 0), head = sg.h * a.G + (live ? row % a.G : 0);
-    const uint16_t* src = a.q + ((int64_t)req * a.Hq + head) * D;
+    const bool live = row < a.G;
+    const uint16_t* src = a.q + ((int64_t)sg.request * a.Hq + sg.h * a.G + (live ? row : 0)) * D;
 #pragma unroll
     for (int s = 0; s < T::kK; ++s) {
       const u32x4 x = *reinterpret_cast<const u32x4*>(src + T::q_at(s, g));
@@ -97,7 +96,7 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, const Pages& pg, con
     }
   }
   const float unit = a.scale * kLog2e * (FP8 && a.k_scale ? a.k_scale[sg.h] : 1.0f);
-  const int32_t* table = pg.table + (int64_t)sg.table_row * pg.max_blocks;
+  const int32_t* table = pg.table + (int64_t)sg.request * pg.max_blocks;
   const int k_first = sg.k0 / kStep * kStep + wave * kStep;
   // a step's pages are looked up one step ahead
   StepPages pages = step_pages(pg, table, k_first);
@@ -158,7 +157,7 @@ __device__ __forceinline__ void merge(const DecodeArgs& a, const Segment& sg, fl
   constexpr int kQuads = D / 4;
   for (int e = threadIdx.x; e < kRows * kQuads; e += kDecodeThreads) {
     const int row = e / kQuads, at = (e % kQuads) * 4;
-    if (sg.row0 + row >= sg.rows) break;
+    if (sg.row0 + row >= a.G) break;
     float mm[kDecodeWaves], top = -INFINITY, sum = 0.0f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -174,10 +173,9 @@ __device__ __forceinline__ void merge(const DecodeArgs& a, const Segment& sg, fl
       sum += f * from[D + 1];
       o += f * *reinterpret_cast<const f32x4*>(from + at);
     }
-    const int i = sg.row0 + row;
-    const int64_t q_row = (int64_t)(sg.first + i / a.G) * a.Hq + sg.h * a.G + i % a.G;
+    const int head = sg.h * a.G + sg.row0 + row;
+    const int64_t q_row = (int64_t)sg.request * a.Hq + head;
     if (whole) {
-      const int head = (int)(q_row % a.Hq);
       if (a.sinks) {
         const float sink = a.sinks[head] * kLog2e, with = fmaxf(top, sink);
         const float f = exp2_fast(top - with);
@@ -221,7 +219,7 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void attn_decode_
     const int lo = own_from(len, reach, a.gr.window), t0 = lo / kTile;
     const int tiles = __builtin_amdgcn_readfirstlane(min(plan.own[r + 1] - v, end - u));
     const bool begins = t == 0, whole = begins && v + tiles == plan.own[r + 1] && reach == 0;
-    Segment sg{r, r, a.G, hv % a.head_tiles * kRows, hv / a.head_tiles, max((t0 + t) * kTile, lo), min((t0 + t + tiles) * kTile, len)};
+    Segment sg{r, hv % a.head_tiles * kRows, hv / a.head_tiles, max((t0 + t) * kTile, lo), min((t0 + t + tiles) * kTile, len)};
     // the same for every lane: keep it in scalar registers
     int* f = reinterpret_cast<int*>(&sg);
 #pragma unroll
@@ -338,10 +336,10 @@ inline bool lds_allowed(const void* kernel, size_t bytes) {
 }
 
 template <int D, bool FP8>
-int launch_decode(const DecodeArgs& a, const Pages& pg, hipStream_t s) {
+int launch_decode(const DecodeArgs& a, const Pages& pg, float* ws, hipStream_t s) {
   using S = SharedTile<D>;
   const int64_t rows = (int64_t)a.gr.R * a.Hq;
-  const Parts parts(a.ws, rows, D, S::kRowsWg);
+  const Parts parts(ws, rows, D, S::kRowsWg);
   const size_t plan = Plan::bytes(a.gr.R, a.gr.n);
   const size_t lds = (size_t)kDecodeWaves * kRows * (D + 4) * 4 + plan;
   if (!lds_allowed(reinterpret_cast<const void*>(attn_decode_kernel<D, FP8>), lds)) return MOE_ERR_HIP;
@@ -402,13 +400,14 @@ extern "C" int moe_attn_decode(const uint16_t* q, const void* k_cache, const voi
   a.q = q, a.k_cache = static_cast<const char*>(k_cache), a.v_cache = static_cast<const char*>(v_cache);
   a.gr = eldr::Groups{lens, group_start, prefix_len, d.R, window > 0 ? 0 : n_groups, window};
   a.k_scale = k_scale, a.v_scale = v_scale, a.sinks = sinks;
-  a.out = out, a.lse = lse, a.ws = static_cast<float*>(ws), a.scale = scale;
+  a.out = out, a.lse = lse, a.scale = scale;
   a.Hq = d.Hq, a.G = d.Hq / d.Hkv, a.head_tiles = (a.G + eldr::kRows - 1) / eldr::kRows;
   eldr::Pages pg = pages_of(d, block_table);
   if (d.num_blocks == 0) pg.max_blocks = 0;  // nothing is cached
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  float* w = static_cast<float*>(ws);
   const bool fp8 = d.kv_type == MOE_KV_FP8;
-  if (d.D == 64) return fp8 ? eldr::launch_decode<64, true>(a, pg, s) : eldr::launch_decode<64, false>(a, pg, s);
-  if (d.D == 128) return fp8 ? eldr::launch_decode<128, true>(a, pg, s) : eldr::launch_decode<128, false>(a, pg, s);
-  return fp8 ? eldr::launch_decode<256, true>(a, pg, s) : eldr::launch_decode<256, false>(a, pg, s);
+  if (d.D == 64) return fp8 ? eldr::launch_decode<64, true>(a, pg, w, s) : eldr::launch_decode<64, false>(a, pg, w, s);
+  if (d.D == 128) return fp8 ? eldr::launch_decode<128, true>(a, pg, w, s) : eldr::launch_decode<128, false>(a, pg, w, s);
+  return fp8 ? eldr::launch_decode<256, true>(a, pg, w, s) : eldr::launch_decode<256, false>(a, pg, w, s);
 }

@@ -77,6 +77,44 @@ struct Keys {
   }
 };
 
+// A 32-slot step of keys by way of LDS: a 16-slot tile is one contiguous stretch
+// of its page, so a wave reads it in whole lines (1 KB a load, where an operand's
+// own load touches 64 pieces of 16 rows), and takes the operands from a stretch
+// of LDS of its own, whose rows are rotated against each other to spread them
+// over the banks.  No barrier: a wave's LDS operations keep their order.
+template <int D, bool FP8>
+struct StagedKeys {
+  using T = Tile<D, FP8>;
+  static constexpr int kRowBytes = D * T::kElem, kChunks = kRowBytes / 16;
+  static constexpr int kTileBytes = 16 * kRowBytes, kLoads = kTileBytes / (16 * kWave);
+  static constexpr int kBytes = 2 * kTileBytes;  // of LDS, a wave
+  u32x4 raw[2][kLoads];
+  static __device__ __forceinline__ uint32_t at(int row, int chunk) {
+    const int turn = kChunks >= 16 ? row & 15 : kChunks == 8 ? (row >> 1) & 7 : (row >> 2) & 3;
+    return (uint32_t)(row * kRowBytes + (chunk ^ turn) * 16);
+  }
+  __device__ __forceinline__ void load(int tile, const char* rows) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      raw[tile][i] = *reinterpret_cast<const u32x4*>(rows + (uint32_t)(threadIdx.x % kWave * 16 + i * 16 * kWave));
+  }
+  // into operands; lds: the wave's kBytes
+  __device__ __forceinline__ void take(char* lds, int n, int g, Keys<D, FP8> (&keys)[2]) const {
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int piece = threadIdx.x % kWave + i * kWave;
+        *reinterpret_cast<u32x4*>(lds + b * kTileBytes + at(piece / kChunks, piece % kChunks)) = raw[b][i];
+      }
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < Keys<D, FP8>::kLoads; ++i)
+        keys[b].raw[i] = *reinterpret_cast<const u32x4*>(lds + b * kTileBytes + at(n, i * 4 + g));
+  }
+};
+
 // 32 slots of values: the lane's kV columns of its 8 slots, 4 of each 16-slot
 // tile (rows 4 g .. 4 g + 3).
 template <int D, bool FP8>

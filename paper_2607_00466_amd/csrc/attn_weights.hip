@@ -24,7 +24,7 @@ constexpr int kWeightWgs = 512;  // two for each CU
 
 // Row tiles of a shared unit, for requests of up to 16 rows: as many as a wave
 // keeps in registers beside a lane's requests in each, 4 / pad.
-constexpr int member_tiles(int D, int pad) { return pad == 1 ? 1 : pad == 2 || D == 256 ? 2 : 4; }
+constexpr int member_tiles(int D, int pad) { return pad == 1 || D == 256 ? 1 : pad == 2 ? 2 : 4; }
 
 struct WeightArgs {
   const uint16_t* q;
@@ -82,13 +82,15 @@ __device__ __forceinline__ void sum_heads(f32x4& x, int in_tile) {
 // The tiles of rows from sp.row0 on, of requests of up to 16 rows; a lane has up
 // to PER requests in a tile, every 4 / PER-th of its rows.
 template <int D, bool FP8, int TILES, int PER>
-__device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, const Span& sp, const int* group) {
+__device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, const Span& sp, const int* group,
+                                      char* stage) {
   using T = Tile<D, FP8>;
   const int lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const float unit = a.scale * kLog2e * (FP8 && a.k_scale ? a.k_scale[sp.h] : 1.0f);
   const int32_t* table = pg.table + (int64_t)sp.table_row * pg.max_blocks;
   const int64_t N = pg.capacity();
+  char* mine_lds = stage + wave * StagedKeys<D, FP8>::kBytes;
   constexpr int kEach = 4 / PER;
   const int64_t next_request = (int64_t)pg.Hkv * N;
   u32x4 q[TILES][T::kK];
@@ -111,10 +113,10 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
     }
   }
   // Steps are asked for kAhead before they are used: keys, and the weights so far.
-  constexpr int kAhead = TILES == 1 ? (D == 256 ? 2 : 3) : (D == 256 ? 1 : 2);
+  constexpr int kAhead = TILES == 1 && D != 256 ? 2 : 1;
   constexpr int kStride = kWeightWaves * kStep;
   struct Set {
-    Keys<D, FP8> keys[2];
+    StagedKeys<D, FP8> keys;
     float before[TILES][2][PER];
     StepPages pages;
   } sets[kAhead];
@@ -125,8 +127,8 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
     s.pages = pages;
     pages = step_pages(pg, table, k + kStride);
     if (k >= sp.k1) return;
-    s.keys[0].template load<false>(a.k_cache + pg.row(pg.has(s.pages.b0) ? s.pages.b0 : 0, sp.h, k) * T::kElem, n, g);
-    s.keys[1].template load<false>(a.k_cache + pg.row(pg.has(s.pages.b1) ? s.pages.b1 : 0, sp.h, k + 16) * T::kElem, n, g);
+    s.keys.load(0, a.k_cache + pg.row(pg.has(s.pages.b0) ? s.pages.b0 : 0, sp.h, k) * T::kElem);
+    s.keys.load(1, a.k_cache + pg.row(pg.has(s.pages.b1) ? s.pages.b1 : 0, sp.h, k + 16) * T::kElem);
     if (a.weights_in) {
       // every lane reads something of the span's rows, so that no load is behind a branch
       const int slots[2] = {k + n, min(k + 16 + n, (int)N - 1)};
@@ -140,13 +142,25 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
   };
   const auto use = [&](Set& st, int k) {
     float sum[TILES][2][PER];
+    Keys<D, FP8> keys[2];
+    st.keys.take(mine_lds, n, g, keys);
+    // the set is free: the step kAhead on is asked for before this one is computed
+    const bool there[2] = {pg.has(st.pages.b0), pg.has(st.pages.b1)};
+    float before[TILES][2][PER];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int c = 0; c < PER; ++c) before[t][b][c] = st.before[t][b][c];
+    fetch(st, k + kAhead * kStride);
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
       f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
       for (int i = 0; i < T::kK; ++i) {
-        s[0] = mfma16x16x32(q[t][i], st.keys[0].operand(i), s[0]);
-        s[1] = mfma16x16x32(q[t][i], st.keys[1].operand(i), s[1]);
+        s[0] = mfma16x16x32(q[t][i], keys[0].operand(i), s[0]);
+        s[1] = mfma16x16x32(q[t][i], keys[1].operand(i), s[1]);
       }
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
@@ -157,10 +171,9 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
         for (int c = 0; c < PER; ++c) sum[t][b][c] = x[c * kEach];
       }
     }
-    const bool there[2] = {pg.has(st.pages.b0), pg.has(st.pages.b1)};
     const auto put = [&](int t, int b, int c) {
       a.weights_out[at[t] + c * next_request + k + n + 16 * b] =
-          (a.weights_in ? st.before[t][b][c] : 0.0f) + (there[b] ? sum[t][b][c] : 0.0f);
+          (a.weights_in ? before[t][b][c] : 0.0f) + (there[b] ? sum[t][b][c] : 0.0f);
     };
     constexpr uint32_t kAll = TILES * PER < 32 ? (1u << (TILES * PER)) - 1 : ~0u;
     if (k >= sp.k0 && k + kStep <= sp.k1 && __all(mine == 0 || mine == kAll)) {
@@ -189,7 +202,6 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
     for (int i = 0; i < kAhead; ++i) {
       if (k + i * kStride >= sp.k1) break;
       use(sets[i], k + i * kStride);
-      fetch(sets[i], k + (i + kAhead) * kStride);
     }
   }
 }
@@ -244,6 +256,7 @@ template <int D, bool FP8>
 __global__ __launch_bounds__(kWeightThreads, 2) void attn_weights_kernel(WeightArgs a, Pages pg, int member_rows) {
   extern __shared__ int lds[];
   __shared__ int waves[kWeightWaves];
+  __shared__ __attribute__((aligned(16))) char stage[kWeightWaves * StagedKeys<D, FP8>::kBytes];
   const int capacity = pg.capacity();
   const Plan plan = make_plan<kWeightThreads>(a.gr, capacity, a.pad, member_rows, lds, waves);
   const int R = a.gr.R, n = a.gr.n, wgs = gridDim.x;
@@ -278,10 +291,10 @@ __global__ __launch_bounds__(kWeightThreads, 2) void attn_weights_kernel(WeightA
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(sp) / 4); ++i) f[i] = __builtin_amdgcn_readfirstlane(f[i]);
     if (a.pad > kRows) weigh_wide<D, FP8>(a, pg, sp, plan.group);
-    else if (sp.group < 0) weigh<D, FP8, 1, 1>(a, pg, sp, plan.group);
-    else if (a.pad == 1) weigh<D, FP8, member_tiles(D, 1), 4>(a, pg, sp, plan.group);
-    else if (a.pad == 2) weigh<D, FP8, member_tiles(D, 2), 2>(a, pg, sp, plan.group);
-    else weigh<D, FP8, member_tiles(D, 4), 1>(a, pg, sp, plan.group);
+    else if (sp.group < 0) weigh<D, FP8, 1, 1>(a, pg, sp, plan.group, stage);
+    else if (a.pad == 1) weigh<D, FP8, member_tiles(D, 1), 4>(a, pg, sp, plan.group, stage);
+    else if (a.pad == 2) weigh<D, FP8, member_tiles(D, 2), 2>(a, pg, sp, plan.group, stage);
+    else weigh<D, FP8, member_tiles(D, 4), 1>(a, pg, sp, plan.group, stage);
     u += __builtin_amdgcn_readfirstlane(tiles);
   }
 }
