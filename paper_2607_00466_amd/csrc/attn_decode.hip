@@ -75,7 +75,7 @@ struct Segment {
 // The running state of 16 rows: maximum and sum (this lane's part) of row
 // lane % 16, and O^T: acc[c][i] is value column (4 (lane / 16) + i) kV + c.
 template <int D, bool FP8>
-__device__ __forceinline__ void attend(const DecodeArgs& a, const Pages& pg, const Segment& sg, float& m, float& l,
+__device__ __forceinline__ void attend(const DecodeArgs& a, const Pages& pg, const Segment& sg, char* stage, float& m, float& l,
                                        f32x4 (&acc)[D / 16]) {
   using T = Tile<D, FP8>;
   const int lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
@@ -106,17 +106,33 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, const Pages& pg, con
     const bool has0 = pg.has(b0), has1 = pg.has(b1);
     const bool whole = has0 && has1 && k >= sg.k0 && k + kStep <= sg.k1;
     const int64_t r0 = pg.row(has0 ? b0 : 0, sg.h, k) * T::kElem, r1 = pg.row(has1 ? b1 : 0, sg.h, k + 16) * T::kElem;
-    Keys<D, FP8> k_lo, k_hi;
+    StagedKeys<D, FP8> staged;
+    Keys<D, FP8> keys[2];
     Values<D, FP8> v;
-    k_lo.template load<true>(a.k_cache + r0, n, g);
-    k_hi.template load<true>(a.k_cache + r1, n, g);
+    // (D = 256 in bf16 has no registers left for the way through LDS)
+    constexpr bool kStaged = D != 256 || FP8;
+    if constexpr (kStaged) {
+      staged.template load<true>(0, a.k_cache + r0);
+      staged.template load<true>(1, a.k_cache + r1);
+    } else {
+      keys[0].template load<true>(a.k_cache + r0, n, g);
+      keys[1].template load<true>(a.k_cache + r1, n, g);
+    }
     v.load(a.v_cache + r0, a.v_cache + r1, n, g);
     __builtin_amdgcn_sched_barrier(0);
+    if constexpr (kStaged) staged.put(stage);
     f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    constexpr int kLoads = Keys<D, FP8>::kLoads, kEach = T::kK / kLoads;
 #pragma unroll
-    for (int i = 0; i < T::kK; ++i) {
-      s[0] = mfma16x16x32(k_lo.operand(i), q[i], s[0]);
-      s[1] = mfma16x16x32(k_hi.operand(i), q[i], s[1]);
+    for (int i = 0; i < kLoads; ++i) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        if constexpr (kStaged) keys[b].raw[i] = StagedKeys<D, FP8>::get(stage, b, i, n, g);
+#pragma unroll
+      for (int e = i * kEach; e < (i + 1) * kEach; ++e) {
+        s[0] = mfma16x16x32(keys[0].operand(e), q[e], s[0]);
+        s[1] = mfma16x16x32(keys[1].operand(e), q[e], s[1]);
+      }
     }
     const auto keep = [&](int j) {
       const int at = k + (j / 4) * 16 + 4 * g + j % 4;
@@ -201,6 +217,10 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void attn_decode_
   extern __shared__ int lds[];
   __shared__ int waves[kDecodeWaves];
   float* sums_lds = reinterpret_cast<float*>(lds);
+  // a wave's keys pass through its own part of where it will leave its sums
+  constexpr int kWaveSums = kRows * (D + 4) * 4;
+  static_assert(StagedKeys<D, FP8>::kBytes <= kWaveSums, "a step's keys fit a wave's sums");
+  char* stage = reinterpret_cast<char*>(lds) + threadIdx.x / kWave * kWaveSums;
   int* plan_lds = lds + kDecodeWaves * kRows * (D + 4);
   const Plan plan = make_plan<kDecodeThreads>(a.gr, pg.capacity(), a.G, SharedTile<D>::kRowsWg, plan_lds, waves);
   const int R = a.gr.R, n = a.gr.n, row = plan.own[R];
@@ -224,7 +244,7 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void attn_decode_
     int* f = reinterpret_cast<int*>(&sg);
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(sg) / 4); ++i) f[i] = __builtin_amdgcn_readfirstlane(f[i]);
-    attend<D, FP8>(a, pg, sg, m, l, acc);
+    attend<D, FP8>(a, pg, sg, stage, m, l, acc);
     merge<D, FP8>(a, sg, m, l, acc, sums_lds, whole,
                   begins ? parts.own : parts.own_rest + (int64_t)blockIdx.x * kRows * (D + 4), begins);
     u += tiles;

@@ -93,13 +93,14 @@ struct StagedKeys {
     const int turn = kChunks >= 16 ? row & 15 : kChunks == 8 ? (row >> 1) & 7 : (row >> 2) & 3;
     return (uint32_t)(row * kRowBytes + (chunk ^ turn) * 16);
   }
+  template <bool STREAM>
   __device__ __forceinline__ void load(int tile, const char* rows) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
-      raw[tile][i] = *reinterpret_cast<const u32x4*>(rows + (uint32_t)(threadIdx.x % kWave * 16 + i * 16 * kWave));
+      raw[tile][i] = tile_load<STREAM, u32x4>(rows + (uint32_t)(threadIdx.x % kWave * 16 + i * 16 * kWave));
   }
-  // into operands; lds: the wave's kBytes
-  __device__ __forceinline__ void take(char* lds, int n, int g, Keys<D, FP8> (&keys)[2]) const {
+  // lds: the wave's kBytes
+  __device__ __forceinline__ void put(char* lds) const {
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -107,11 +108,10 @@ struct StagedKeys {
         const int piece = threadIdx.x % kWave + i * kWave;
         *reinterpret_cast<u32x4*>(lds + b * kTileBytes + at(piece / kChunks, piece % kChunks)) = raw[b][i];
       }
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int i = 0; i < Keys<D, FP8>::kLoads; ++i)
-        keys[b].raw[i] = *reinterpret_cast<const u32x4*>(lds + b * kTileBytes + at(n, i * 4 + g));
+  }
+  // Keys::raw[i] of tile b
+  static __device__ __forceinline__ u32x4 get(const char* lds, int b, int i, int n, int g) {
+    return *reinterpret_cast<const u32x4*>(lds + b * kTileBytes + at(n, i * 4 + g));
   }
 };
 

@@ -127,8 +127,8 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
     s.pages = pages;
     pages = step_pages(pg, table, k + kStride);
     if (k >= sp.k1) return;
-    s.keys.load(0, a.k_cache + pg.row(pg.has(s.pages.b0) ? s.pages.b0 : 0, sp.h, k) * T::kElem);
-    s.keys.load(1, a.k_cache + pg.row(pg.has(s.pages.b1) ? s.pages.b1 : 0, sp.h, k + 16) * T::kElem);
+    s.keys.template load<false>(0, a.k_cache + pg.row(pg.has(s.pages.b0) ? s.pages.b0 : 0, sp.h, k) * T::kElem);
+    s.keys.template load<false>(1, a.k_cache + pg.row(pg.has(s.pages.b1) ? s.pages.b1 : 0, sp.h, k + 16) * T::kElem);
     if (a.weights_in) {
       // every lane reads something of the span's rows, so that no load is behind a branch
       const int slots[2] = {k + n, min(k + 16 + n, (int)N - 1)};
@@ -143,7 +143,11 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
   const auto use = [&](Set& st, int k) {
     float sum[TILES][2][PER];
     Keys<D, FP8> keys[2];
-    st.keys.take(mine_lds, n, g, keys);
+    st.keys.put(mine_lds);
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < Keys<D, FP8>::kLoads; ++i) keys[b].raw[i] = StagedKeys<D, FP8>::get(mine_lds, b, i, n, g);
     // the set is free: the step kAhead on is asked for before this one is computed
     const bool there[2] = {pg.has(st.pages.b0), pg.has(st.pages.b1)};
     float before[TILES][2][PER];
