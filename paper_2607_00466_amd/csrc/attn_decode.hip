@@ -10,15 +10,15 @@
 //
 // The reduction over slots may take them in any order that both operands share,
 // so the second product's slot order is chosen to be the one in which a lane
-// holds P already: no shuffle and no LDS between the two products.  Keys and
-// values go from HBM to registers directly: a lane loads 16 bytes of one row,
-// and a value tile is transposed inside the lane (its rows' 16-bit halves are
-// zipped by v_perm).  What bounds it is HBM, by loads that do not displace what
-// the caches hold (non-temporal; 203 -> 178 us in the first case below).  Measured:
-// 128 requests of up to 8000 tokens (32 heads over 4 of 128, bf16) 175 us, 6.3 TB/s
-// of a streaming read's 7.05; 64 x 16384 in fp8 174 us; D = 64 339 us and D = 256
-// 355 us for 2.1 GB.  Dealing the units to waves in place of workgroups (no merge in
-// LDS, four times the parts) measured 2 to 8% slower.
+// holds P already: no shuffle and no LDS between the two products.  Rows are read
+// in whole lines, a value tile transposed inside the lane (its rows' 16-bit halves
+// are zipped by v_perm), a key tile handed over through LDS.  What bounds it is
+// HBM; the loads are non-temporal, so that they do not displace what the caches
+// hold (203 -> 178 us in the first case below).  Measured: 128 requests of up to
+// 8000 tokens (32 heads over 4 of 128, bf16, 1.1 GB) 177 us, 6.3 TB/s of a
+// streaming read's 7.05; 64 of 16384 in fp8 (1.1 GB) 166; D = 64 331 us and D = 256
+// 353 us for 2.1 GB.  Dealing the units to waves in place of workgroups (no merge
+// in LDS, four times the parts) measured 2 to 8% slower.
 //
 // The four waves of a workgroup take turns at a segment's 32-slot steps and
 // meet in LDS at its end.  A segment that is a request's whole context gives

@@ -12,6 +12,13 @@
 //
 // The products and the softmax are as in the other kernel: S^T = K Q^T, weights
 // used where the product left them.
+//
+// Measured: 64 requests (32 heads over 4 of 128) against 8192 shared slots 25 us,
+// against 65536 113 us (610 TFLOP/s): a stage takes a workgroup 1.5 us, of which
+// its two waves a SIMD spend half in MFMAs and exponents and the rest in the
+// dependences between them; starting (plan, queries, first stage) takes 6 us and
+// handing over the parts 3.  Stages of 128 slots measured the same (4% faster at
+// D = 64), more stages in flight too.
 #pragma once
 
 #include "attn_plan.hpp"

@@ -12,7 +12,10 @@
 // A unit is 128 slots of one request, or of a group against up to kMemberTiles
 // tiles of its members' rows, dealt out as for moe_attn_decode.  A wave keeps its
 // rows' queries and lse in registers and takes 32 slots at a time, the next ones'
-// keys on their way.  Bound by HBM: keys once, weights in and out.
+// keys on their way.  Own slots are bound by HBM: keys once, weights in and out
+// (64 requests of up to 4000 tokens, 149 MB, 31 us, 4.8 TB/s; 64 of 16384 206 us,
+// 6.5 TB/s).  A prefix is not: 64 requests behind 8192 slots take 33 us where the
+// bytes take 10, with stores, exponents or the keys' misses left out nearly as long.
 #include "attn_plan.hpp"
 #include "attn_tile.hpp"
 

@@ -7,7 +7,9 @@
 // pair are in one thread.  Where there are tokens enough to fill the chip, a
 // thread does so for several heads with the angles it has read once: a token's
 // angles are as many bytes as a head's values.  Bound by bytes for a prompt and
-// by two dependent loads (position, then table) for a decode batch.
+// by two dependent loads (position, then table) for a decode batch.  Measured: 4096
+// tokens of 40 heads of 128 in fp32 25 us (5.0 TB/s, a large copy's rate; 54 us with
+// a head a thread), 64 tokens in bf16 3.7 us.
 #include "attn_common.hpp"
 
 namespace eldr {

@@ -13,6 +13,11 @@
 // it, so no row is both read and written and the copies need no order.  Where a
 // row can be over its budget by 64 slots at most, as when every step evicts what
 // it appended, kv_select copies them itself and there is no second launch.
+//
+// Measured: 256 caches of 4 heads, one token each past 1024, 16.6 us (a lane's
+// loads, four barriers and the launch; 43 us with keys read again for each digit);
+// 64 of up to 4096 cut to 2048 15 us and the move 35 (172 MB, 4.9 TB/s, a large
+// copy's rate).
 #include "attn_common.hpp"
 
 namespace eldr {
