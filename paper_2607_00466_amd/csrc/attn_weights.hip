@@ -37,6 +37,7 @@ struct WeightArgs {
   float* weights_out;
   float scale;
   int32_t Hq, G, pad;  // pad: rows a request takes, a power of two up to 16 or a multiple of 16
+  int32_t pad_shift;   // of the former
 };
 
 // Requests [first, end), of which those in `group` (-1: all) count; rows
@@ -50,15 +51,21 @@ struct Span {
 template <int D, bool FP8>
 __device__ __forceinline__ void load_rows(const WeightArgs& a, const Span& sp, int row0, u32x4 (&q)[D / 32], f32x4& lse) {
   const int lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
-  const int row = row0 + n, req = sp.first + row / a.pad, i = row % a.pad;
-  const bool live = i < a.G && req < sp.end;
-  const uint16_t* src = a.q + ((int64_t)(live ? req : sp.first) * a.Hq + sp.h * a.G + (live ? i : 0)) * D;
+  const auto request = [&](int row) { return sp.first + (a.pad <= kRows ? row >> a.pad_shift : row / a.pad); };
+  const auto head = [&](int row) { return a.pad <= kRows ? row & (a.pad - 1) : row % a.pad; };
+  {
+    const int req = request(row0 + n), i = head(row0 + n);
+    const uint16_t* src = a.q + ((int64_t)min(req, sp.end - 1) * a.Hq + sp.h * a.G + (i < a.G ? i : 0)) * D;
 #pragma unroll
-  for (int s = 0; s < D / 32; ++s) q[s] = *reinterpret_cast<const u32x4*>(src + Tile<D, FP8>::q_at(s, g));
+    for (int s = 0; s < D / 32; ++s) q[s] = *reinterpret_cast<const u32x4*>(src + Tile<D, FP8>::q_at(s, g));
+  }
+  // (what does not count is set by bits: a select would put each load behind a branch, one wait after another)
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
-    const int rr = row0 + 4 * g + c, r = sp.first + rr / a.pad, j = rr % a.pad;
-    lse[c] = j < a.G && r < sp.end ? a.lse[(int64_t)r * a.Hq + sp.h * a.G + j] * kLog2e : INFINITY;
+    const int r = request(row0 + 4 * g + c), i = head(row0 + 4 * g + c);
+    const float x = a.lse[(int64_t)min(r, sp.end - 1) * a.Hq + sp.h * a.G + (i < a.G ? i : 0)] * kLog2e;
+    const uint32_t live = i < a.G && r < sp.end ? 0xffffffffu : 0u;
+    lse[c] = __uint_as_float((__float_as_uint(x) & live) | (__float_as_uint(INFINITY) & ~live));
   }
 }
 
@@ -106,13 +113,13 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
     const int row0 = sp.row0 + t * kRows;
     load_rows<D, FP8>(a, sp, row0, q[t], lse[t]);
     // (kept within the span's requests, so that what it names can always be read)
-    const int first = min(sp.first + (row0 + 4 * g) / a.pad, sp.end - 1);
+    const int first = min(sp.first + ((row0 + 4 * g) >> a.pad_shift), sp.end - 1);
     at[t] = ((int64_t)first * pg.Hkv + sp.h) * N;
     past[t] = sp.end - 1 - first;
 #pragma unroll
     for (int c = 0; c < PER; ++c) {
-      const int row = row0 + 4 * g + c * kEach, r = sp.first + row / a.pad;
-      if (row % a.pad == 0 && row < sp.row1 && r < sp.end && (sp.group < 0 || group[r] == sp.group)) mine |= 1u << (PER * t + c);
+      const int row = row0 + 4 * g + c * kEach, r = sp.first + (row >> a.pad_shift);
+      if ((row & (a.pad - 1)) == 0 && row < sp.row1 && r < sp.end && (sp.group < 0 || group[r] == sp.group)) mine |= 1u << (PER * t + c);
     }
   }
   // Steps are asked for kAhead before they are used: keys, and the weights so far.
@@ -341,6 +348,7 @@ extern "C" int moe_attn_weights(const uint16_t* q, const void* k_cache, const in
   a.pad = 1;
   while (a.pad < a.G && a.pad < eldr::kRows) a.pad *= 2;
   if (a.G > eldr::kRows) a.pad = (a.G + eldr::kRows - 1) / eldr::kRows * eldr::kRows;
+  a.pad_shift = __builtin_ctz((unsigned)a.pad);
   const eldr::Pages pg = pages_of(d, block_table);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const bool fp8 = d.kv_type == MOE_KV_FP8;
