@@ -49,8 +49,6 @@ __device__ __forceinline__ int wave_sum_before(int x) {
   return x;
 }
 
-__device__ __forceinline__ float bf16_to_float(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
-
 // Round to nearest even; two values in one word, the first in the low half.
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
