@@ -78,6 +78,8 @@ def decode(q, k_cache, v_cache, table, lens, scale, group_start=None, prefix_len
             if not len(every):
                 continue
             top = every.max()
+            if top == -np.inf:  # the sum is 0: as without a visible slot
+                continue
             lse[r, h] = top + np.log(np.exp(every - top).sum())
             if vis:
                 p = np.exp(s - lse[r, h])

@@ -154,6 +154,31 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, const Pages& pg, con
   l += __shfl_xor(l, 32);
 }
 
+// A row's end: what gives the output from its sums of values, and its lse.
+struct RowEnd {
+  float by, lse;
+};
+
+// From a row's maximum (in base-2 units) and sum; sink: the row's, or null; unit:
+// the values' scale.  The sink is weighed in its own units, where the difference
+// that counts can be taken of any finite value: the lowest one, in base 2, would be
+// -inf already.  Where it and the maximum are both -inf there is nothing to weigh:
+// the reference stays finite, so that the sums stay zero.
+__device__ __forceinline__ RowEnd end_row(float top, float total, const float* sink, float unit) {
+  constexpr float kLn2 = 0.6931471805599453f;
+  const float own = top * kLn2;
+  float with = own, f = 1.0f;
+  if (sink) {
+    with = fmaxf(own, *sink);
+    const float base = with == -INFINITY ? 0.0f : with;
+    f = exp2_fast((own - base) * kLog2e);
+    total = total * f + exp2_fast((*sink - base) * kLog2e);
+  }
+  if (!(total > 0.0f)) return RowEnd{0.0f, -INFINITY};
+  const float log2_total = __builtin_amdgcn_logf(total);
+  return RowEnd{f * unit / total, sink ? with + log2_total * kLn2 : (top + log2_total) * kLn2};
+}
+
 // Adds the four waves' states in LDS; then writes the rows' sums as a part, or
 // as the output.  lds: kDecodeWaves * kRows * (D + 4) floats.
 template <int D, bool FP8>
@@ -192,17 +217,10 @@ __device__ __forceinline__ void merge(const DecodeArgs& a, const Segment& sg, fl
     const int head = sg.h * a.G + sg.row0 + row;
     const int64_t q_row = (int64_t)sg.request * a.Hq + head;
     if (whole) {
-      if (a.sinks) {
-        const float sink = a.sinks[head] * kLog2e, with = fmaxf(top, sink);
-        const float f = exp2_fast(top - with);
-        sum = sum * f + exp2_fast(sink - with);
-        o *= f;
-        top = with;
-      }
-      const float by = sum > 0.0f ? (FP8 && a.v_scale ? a.v_scale[sg.h] : 1.0f) / sum : 0.0f;
-      *reinterpret_cast<u32x2*>(a.out + q_row * D + at) = u32x2{pack_bf16(o[0] * by, o[1] * by), pack_bf16(o[2] * by, o[3] * by)};
-      if (at == 0 && a.lse)
-        a.lse[q_row] = sum > 0.0f ? (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
+      const RowEnd end = end_row(top, sum, a.sinks ? a.sinks + head : nullptr, FP8 && a.v_scale ? a.v_scale[sg.h] : 1.0f);
+      o *= end.by;
+      *reinterpret_cast<u32x2*>(a.out + q_row * D + at) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+      if (at == 0 && a.lse) a.lse[q_row] = end.lse;
     } else {
       float* to = part + (by_row ? q_row : (int64_t)row) * (D + 4);
       *reinterpret_cast<f32x4*>(to + at) = o;
@@ -334,17 +352,10 @@ __global__ __launch_bounds__(kDecodeThreads) void attn_join_kernel(DecodeArgs a,
     sum = sum * f + sums[s][at] * e;
     top = m2;
   }
-  if (a.sinks) {
-    const float sink = a.sinks[hq] * kLog2e, with = fmaxf(top, sink), f = exp2_fast(top - with);
-    total = total * f + exp2_fast(sink - with);
-    sum *= f;
-    top = with;
-  }
-  const float by = total > 0.0f ? (FP8 && a.v_scale ? a.v_scale[h] : 1.0f) / total : 0.0f;
-  *reinterpret_cast<u32x2*>(a.out + (int64_t)q_row * D + 4 * at) =
-      u32x2{pack_bf16(sum[0] * by, sum[1] * by), pack_bf16(sum[2] * by, sum[3] * by)};
-  if (at == 0 && a.lse)
-    a.lse[q_row] = total > 0.0f ? (top + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+  const RowEnd end = end_row(top, total, a.sinks ? a.sinks + hq : nullptr, FP8 && a.v_scale ? a.v_scale[h] : 1.0f);
+  sum *= end.by;
+  *reinterpret_cast<u32x2*>(a.out + (int64_t)q_row * D + 4 * at) = u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
+  if (at == 0 && a.lse) a.lse[q_row] = end.lse;
 }
 
 // Raises a kernel's dynamic LDS limit where a launch needs more than the default.
