@@ -163,10 +163,12 @@ struct RowEnd {
 // the values' scale.  The sink is weighed in its own units, where the difference
 // that counts can be taken of any finite value: the lowest one, in base 2, would be
 // -inf already.  Where it and the maximum are both -inf there is nothing to weigh:
-// the reference stays finite, so that the sums stay zero.
+// the reference stays finite, so that the sums stay zero.  A row is empty where its
+// sum is 0, and only there: a sum that is NaN gives NaN.
 __device__ __forceinline__ RowEnd end_row(float top, float total, const float* sink, float unit) {
   constexpr float kLn2 = 0.6931471805599453f;
   const float own = top * kLn2;
+  const bool empty = total == 0.0f;
   float with = own, f = 1.0f;
   if (sink) {
     with = fmaxf(own, *sink);
@@ -174,9 +176,8 @@ __device__ __forceinline__ RowEnd end_row(float top, float total, const float* s
     f = exp2_fast((own - base) * kLog2e);
     total = total * f + exp2_fast((*sink - base) * kLog2e);
   }
-  if (!(total > 0.0f)) return RowEnd{0.0f, -INFINITY};
-  const float log2_total = __builtin_amdgcn_logf(total);
-  return RowEnd{f * unit / total, sink ? with + log2_total * kLn2 : (top + log2_total) * kLn2};
+  const float log2_total = __builtin_amdgcn_logf(total);  // -inf where there is neither a slot nor a sink
+  return RowEnd{empty ? 0.0f : f * unit / total, sink ? with + log2_total * kLn2 : (top + log2_total) * kLn2};
 }
 
 // Adds the four waves' states in LDS; then writes the rows' sums as a part, or
