@@ -337,7 +337,8 @@ __global__ __launch_bounds__(kDecodeThreads) void attn_join_kernel(DecodeArgs a,
       const float m2 = fmaxf(top, pm), base = m2 == -INFINITY ? 0.0f : m2;
       const float f = exp2_fast(top - base), e = exp2_fast(pm - base);
       total = total * f + ml[b][1] * e;
-      sum = sum * f + v[b] * e;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] = sum[i] * f + (there ? v[b][i] : 0.0f) * e;  // (0 times what is not there may be NaN)
       top = m2;
     }
   }
