@@ -50,9 +50,10 @@
  * group_start [n_groups + 1] and prefix_len [n_groups] (int32, on the device):
  * requests group_start[g] .. group_start[g + 1] - 1 hold the same tokens in
  * slots [0, prefix_len[g]), and those are read through the block table row of
- * the group's first request, once for the group.  (The slots are shared as far
- * as the shortest non-empty member reaches; past that, and in a group of one,
- * each request reads its own row.)  group_start must not descend; it is taken
+ * the group's first request that holds anything (lens > 0), once for the group.
+ * (The slots are shared as far as the shortest non-empty member reaches; past
+ * that, and in a group of one, each request reads its own row.  An empty
+ * member's row is not read.)  group_start must not descend; it is taken
  * as clamped to [0, R], and requests outside every group share nothing.
  * n_groups = 0: nothing is shared and both pointers may be NULL.
  */

@@ -27,7 +27,8 @@ def rotate(x, positions, pair_axis, cos, sin, interleaved=False):
 
 
 def shared_reach(lens, group_start, prefix_len, N, window=0):
-    """For each request, (first request of its group, slots read through that one)."""
+    """For each request, (first request of its group that holds anything, slots read
+    through that one)."""
     R = len(lens)
     lens = np.clip(lens, 0, N)
     out = [(r, 0) for r in range(R)]
@@ -36,11 +37,11 @@ def shared_reach(lens, group_start, prefix_len, N, window=0):
     s = min(max(int(group_start[0]), 0), R)
     for g in range(len(prefix_len)):
         e = min(max(int(group_start[g + 1]), s), R)
-        full = [int(lens[r]) for r in range(s, e) if lens[r] > 0]
-        reach = min([min(max(int(prefix_len[g]), 0), N)] + full)
+        full = [r for r in range(s, e) if lens[r] > 0]
+        reach = min([min(max(int(prefix_len[g]), 0), N)] + [int(lens[r]) for r in full])
         if e - s > 1:
             for r in range(s, e):
-                out[r] = (s, reach)
+                out[r] = (full[0] if full else s, reach)
         s = e
     return out
 

@@ -30,7 +30,7 @@ struct Plan {
   int *reach;   // [R] slots read with the group
   int *group;   // [R] the request's group, -1: none
   int *shared;  // [n + 1] shared units (row tiles x slot tiles) before each group
-  int *least;   // [n] slots the group shares
+  int *first;   // [n] the group's first request that holds anything: the prefix is read through its row (R: none does)
   int *len;     // [R] cached slots
   int *start;   // [n + 1] the groups' first requests
 
@@ -82,12 +82,16 @@ __device__ __forceinline__ Plan make_plan(const Groups& gr, int capacity, int G,
   p.reach = p.own + gr.R + 1;
   p.group = p.reach + gr.R;
   p.shared = p.group + gr.R;
-  p.least = p.shared + gr.n + 1;
-  p.len = p.least + gr.n;
+  p.first = p.shared + gr.n + 1;
+  p.len = p.first + gr.n;
   p.start = p.len + gr.R;
+  // until the requests know their reach: the slots that a group shares where `first`
+  // will be, and the first request where `shared` will be
+  int *least = p.first, *holder = p.shared;
   for (int r = threadIdx.x; r < gr.R; r += THREADS) p.len[r] = clamp_len(gr.lens[r], capacity);
   for (int g = threadIdx.x; g < gr.n; g += THREADS) {
-    p.least[g] = clamp_len(gr.prefix[g], capacity);
+    least[g] = clamp_len(gr.prefix[g], capacity);
+    holder[g] = gr.R;
     p.start[g] = min(max(gr.start[g], 0), gr.R);
   }
   if (gr.n > 0 && threadIdx.x == 0) p.start[gr.n] = min(max(gr.start[gr.n], 0), gr.R);
@@ -103,23 +107,27 @@ __device__ __forceinline__ Plan make_plan(const Groups& gr, int capacity, int G,
         else hi = mid;
       }
       const int s = p.start[lo], e = p.start[lo + 1];
-      // an empty member reads nothing and does not shorten what the others share
+      // an empty member reads nothing, does not shorten what the others share, and
+      // its row of the block table may name anything
       if (s <= r && r < e && e - s > 1 && p.len[r] > 0) {
         group = lo;
-        atomicMin(&p.least[lo], p.len[r]);
+        atomicMin(&least[lo], p.len[r]);
+        if (r == s || p.len[r - 1] == 0) atomicMin(&holder[lo], r);  // (a member that follows one that holds something is not the first)
       }
     }
     p.group[r] = group;
   }
   __syncthreads();
-  for (int r = threadIdx.x; r < gr.R; r += THREADS) p.reach[r] = p.group[r] < 0 ? 0 : p.least[p.group[r]];
+  for (int r = threadIdx.x; r < gr.R; r += THREADS) p.reach[r] = p.group[r] < 0 ? 0 : least[p.group[r]];
   __syncthreads();
+  for (int g = threadIdx.x; g < gr.n; g += THREADS) p.first[g] = holder[g];
+  // (a barrier of the sums comes before `first` is read and `shared` written)
   sums<THREADS>(gr.R, p.own, waves,
                 [&](int r) { return tiles_of(own_from(p.len[r], p.reach[r], gr.window), p.len[r]); });
   if (gr.n > 0)
     sums<THREADS>(gr.n, p.shared, waves, [&](int g) {
       const int members = p.start[g + 1] - p.start[g];
-      return members > 1 ? (members * G + row_tile - 1) / row_tile * tiles_of(0, p.least[g]) : 0;
+      return p.first[g] < gr.R ? (members * G + row_tile - 1) / row_tile * tiles_of(0, p.reach[p.first[g]]) : 0;
     });
   else if (threadIdx.x == 0)
     p.shared[0] = 0;

@@ -91,10 +91,11 @@ struct SharedArgs {
   int32_t Hq, G;
 };
 
-// Rows [row0, row0 + kRowsWg) of a group's members on kv head h, against slots
-// [k0, k1) of the prefix; k0 is a multiple of kTile.
+// Rows [row0, row0 + kRowsWg) of a group's members (requests from `first` on) on kv
+// head h, against slots [k0, k1) of the prefix, through row table_row of the block
+// table; k0 is a multiple of kTile.
 struct SharedSegment {
-  int table_row, rows, row0, h, k0, k1;
+  int first, table_row, rows, row0, h, k0, k1;
 };
 
 template <int D, bool FP8>
@@ -112,7 +113,7 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
   for (int t = 0; t < S::kQ; ++t) {
     const int row = wave_row + t * kRows + n;
     const bool there = row < sg.rows;
-    const int req = sg.table_row + (there ? row / a.G : 0), head = sg.h * a.G + (there ? row % a.G : 0);
+    const int req = sg.first + (there ? row / a.G : 0), head = sg.h * a.G + (there ? row % a.G : 0);
     const uint16_t* src = a.q + ((int64_t)req * a.Hq + head) * D;
 #pragma unroll
     for (int s = 0; s < kK; ++s) {
@@ -300,7 +301,7 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
   const int live_rows = min(S::kRowsWg, sg.rows - sg.row0);
   for (int e = threadIdx.x; e < live_rows * kQuads; e += kSharedThreads) {
     const int r = e / kQuads, row = sg.row0 + r;
-    const int64_t q_row = (int64_t)(sg.table_row + row / a.G) * a.Hq + sg.h * a.G + row % a.G;
+    const int64_t q_row = (int64_t)(sg.first + row / a.G) * a.Hq + sg.h * a.G + row % a.G;
     *reinterpret_cast<f32x4*>(part + (by_row ? q_row : (int64_t)r) * kPitch + (e - r * kQuads) * 4) =
         *reinterpret_cast<const f32x4*>(tile + e * 4);
   }
@@ -324,10 +325,10 @@ __global__ __launch_bounds__(kSharedThreads, 2) void attn_shared_kernel(SharedAr
     const int h = u / row, v = u - h * row;
     const int grp = last_at(plan.shared, n, v);
     const int first = plan.start[grp], members = plan.start[grp + 1] - first;
-    const int reach = plan.least[grp], per = tiles_of(0, reach), in = v - plan.shared[grp];
+    const int table_row = plan.first[grp], reach = plan.reach[table_row], per = tiles_of(0, reach), in = v - plan.shared[grp];
     const int tile = in / per, t = in - tile * per;
     const int tiles = __builtin_amdgcn_readfirstlane(min(per - t, end - u));
-    SharedSegment sg{first, members * a.G, tile * S::kRowsWg, h, t * kTile, min((t + tiles) * kTile, reach)};
+    SharedSegment sg{first, table_row, members * a.G, tile * S::kRowsWg, h, t * kTile, min((t + tiles) * kTile, reach)};
     int* f = reinterpret_cast<int*>(&sg);
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(sg) / 4); ++i) f[i] = __builtin_amdgcn_readfirstlane(f[i]);

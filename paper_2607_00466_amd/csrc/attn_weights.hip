@@ -43,7 +43,8 @@ struct WeightArgs {
 };
 
 // Requests [first, end), of which those in `group` (-1: all) count; rows
-// [row0, row1) of their padded heads; slots [k0, k1).
+// [row0, row1) of their padded heads; slots [k0, k1), through row table_row of the
+// block table.
 struct Span {
   int table_row, first, end, group, row0, row1, h, k0, k1;
 };
@@ -290,10 +291,10 @@ __global__ __launch_bounds__(kWeightThreads, 2) void attn_weights_kernel(WeightA
     if (u < shared_units) {
       const int h = u / shared_row, v = u - h * shared_row;
       const int grp = last_at(plan.shared, n, v);
-      const int first = plan.start[grp], last = plan.start[grp + 1], reach = plan.least[grp];
+      const int first = plan.start[grp], last = plan.start[grp + 1], table_row = plan.first[grp], reach = plan.reach[table_row];
       const int per = tiles_of(0, reach), in = v - plan.shared[grp], run = in / per, t = in - run * per;
       tiles = min(per - t, end - u);
-      sp = Span{first, first, last, grp, run * member_rows, min((run + 1) * member_rows, (last - first) * a.pad), h,
+      sp = Span{table_row, first, last, grp, run * member_rows, min((run + 1) * member_rows, (last - first) * a.pad), h,
                 t * kTile, min((t + tiles) * kTile, reach)};
     } else {
       const int o = u - shared_units, h = o / own_row, v = o - h * own_row;
