@@ -49,6 +49,15 @@ __device__ __forceinline__ int wave_sum_before(int x) {
   return x;
 }
 
+// Between LDS that some lanes of a wave wrote and other lanes of it read, or the
+// other way round.  The hardware keeps a wave's LDS operations in order, so no wait
+// comes of this: it keeps the compiler from moving one of them past it.
+__device__ __forceinline__ void wave_handover() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // Round to nearest even; two values in one word, the first in the low half.
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));

@@ -189,6 +189,7 @@ __device__ __forceinline__ void merge(const DecodeArgs& a, const Segment& sg, fl
   constexpr int kV = D / 16;
   const int lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16, wave = threadIdx.x / kWave;
   float* mine = lds + (wave * kRows + n) * kPitch;
+  wave_handover();  // the wave's last keys lay here
   if (g == 0) mine[D] = m, mine[D + 1] = l;
 #pragma unroll
   for (int i = 0; i < 4; ++i)

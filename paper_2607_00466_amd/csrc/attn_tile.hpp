@@ -81,7 +81,7 @@ struct Keys {
 // of its page, so a wave reads it in whole lines (1 KB a load, where an operand's
 // own load touches 64 pieces of 16 rows), and takes the operands from a stretch
 // of LDS of its own, whose rows are rotated against each other to spread them
-// over the banks.  No barrier: a wave's LDS operations keep their order.
+// over the banks.  No barrier of the workgroup: the stretch is one wave's.
 template <int D, bool FP8>
 struct StagedKeys {
   using T = Tile<D, FP8>;
@@ -101,6 +101,7 @@ struct StagedKeys {
   }
   // lds: the wave's kBytes
   __device__ __forceinline__ void put(char* lds) const {
+    wave_handover();  // after the last step's operands
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -108,6 +109,7 @@ struct StagedKeys {
         const int piece = threadIdx.x % kWave + i * kWave;
         *reinterpret_cast<u32x4*>(lds + b * kTileBytes + at(piece / kChunks, piece % kChunks)) = raw[b][i];
       }
+    wave_handover();
   }
   // Keys::raw[i] of tile b
   static __device__ __forceinline__ u32x4 get(const char* lds, int b, int i, int n, int g) {
