@@ -142,7 +142,8 @@ int moe_kv_append(const void* q, const void* k, const void* v, int64_t q_stride,
  * visible slot gets out = 0 and lse = -inf, or the sink's value; a sink of -inf
  * weighs nothing.  A NaN that counts (in a query, a visible row or a sink) gives
  * NaN.  Where window > 0 no prefix is shared.  Scores, statistics and sums are
- * fp32; a weight is rounded to bf16 as it enters the product with v.  The result
+ * fp32; a weight enters the product with v in two bf16 parts, 16 bits of it, so
+ * that out's error is that of its own rounding.  The result
  * does not depend on anything but the arguments' values (no atomics on floats);
  * how a long request is split depends on the whole batch's lengths, so a
  * request's last bits may differ between batches.

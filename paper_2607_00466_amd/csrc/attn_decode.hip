@@ -6,7 +6,8 @@
 //
 //   S^T = K Q^T   two 16x16 tiles of (slot, row), MFMA over D
 //   P   = exp2(S^T - m), in the lanes that the products left it in
-//   O^T += V^T P  MFMA over the 32 slots
+//   O^T += V^T P  MFMA over the 32 slots, P in two bf16 parts: the matrix cores
+//                 have the time (all attend cases without groups within 1%)
 //
 // The reduction over slots may take them in any order that both operands share,
 // so the second product's slot order is chosen to be the one in which a lane
@@ -142,12 +143,16 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, const Pages& pg, con
 #pragma unroll
       for (int j = 0; j < 8; ++j) v.drop(j, keep(j));
     }
-    const u32x4 p = softmax_step(s, unit, whole, keep, m, l, [&](float f) {
+    const Weights p = softmax_step(s, unit, whole, keep, m, l, [&](float f) {
 #pragma unroll
       for (int c = 0; c < T::kV; ++c) acc[c] *= f;
     });
 #pragma unroll
-    for (int c = 0; c < T::kV; ++c) acc[c] = mfma16x16x32(v.operand(c), p, acc[c]);
+    for (int c = 0; c < T::kV; ++c) {
+      const u32x4 x = v.operand(c);
+      acc[c] = mfma16x16x32(x, p.most, acc[c]);
+      acc[c] = mfma16x16x32(x, p.rest, acc[c]);
+    }
   }
   // the row's sum over the four lanes that share it
   l += __shfl_xor(l, 16);

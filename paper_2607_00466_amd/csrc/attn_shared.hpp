@@ -11,7 +11,9 @@
 // each workgroup leaves a part of every row it held.
 //
 // The products and the softmax are as in the other kernel: S^T = K Q^T, weights
-// used where the product left them.
+// used where the product left them, in two bf16 parts.  (Here the second part's
+// product costs: 64 behind 8192 48.8 -> 51.5 us, 64 behind 65536 127 -> 144, the
+// whole call; with one part these outputs' error was 1.3 times their rounding's.)
 //
 // Measured: 64 requests (32 heads over 4 of 128) against 8192 shared slots 25 us,
 // against 65536 113 us (610 TFLOP/s): a stage takes a workgroup 1.5 us, of which
@@ -207,13 +209,15 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
       }
       const bool whole = (there & 3u) == 3u && k_mine + kStep <= sg.k1;
       const auto keep = [&](int j) { return (there >> (j / 4) & 1u) && k_mine + (j / 4) * 16 + 4 * g + j % 4 < sg.k1; };
-      u32x4 p[S::kQ];
+      u32x4 most[S::kQ], rest[S::kQ];
 #pragma unroll
-      for (int t = 0; t < S::kQ; ++t)
-        p[t] = softmax_step(s[t], unit, whole, keep, m[t], l[t], [&](float f) {
+      for (int t = 0; t < S::kQ; ++t) {
+        const Weights p = softmax_step(s[t], unit, whole, keep, m[t], l[t], [&](float f) {
 #pragma unroll
           for (int c = 0; c < kV; ++c) acc[t][c] *= f;
         });
+        most[t] = p.most, rest[t] = p.rest;
+      }
       // eight value columns a lane at a time (four where D is 64)
       constexpr int kCols = kV < 8 ? kV : 8;
 #pragma unroll
@@ -236,7 +240,9 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
         for (int c = 0; c < kCols; ++c) {
           const u32x4 x = v.operand(c);
 #pragma unroll
-          for (int t = 0; t < S::kQ; ++t) acc[t][w * kCols + c] = mfma16x16x32(x, p[t], acc[t][w * kCols + c]);
+          for (int t = 0; t < S::kQ; ++t) acc[t][w * kCols + c] = mfma16x16x32(x, most[t], acc[t][w * kCols + c]);
+#pragma unroll
+          for (int t = 0; t < S::kQ; ++t) acc[t][w * kCols + c] = mfma16x16x32(x, rest[t], acc[t][w * kCols + c]);
         }
       }
     }
