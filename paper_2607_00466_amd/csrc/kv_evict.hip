@@ -10,14 +10,19 @@
 // leaves below the budget with the i-th that stays past it.
 //
 // kv_move copies those rows: sources lie past the budget and destinations below
-// it, so no row is both read and written and the copies need no order.  Where a
-// row can be over its budget by 64 slots at most, as when every step evicts what
-// it appended, kv_select copies them itself and there is no second launch.
+// it, so no row is both read and written and the copies need no order.  Where the
+// table holds no more than 64 slots over the budget (one made for the budget and for
+// what the steps append), kv_select copies them itself and there is no second launch.
+// Both choices go by the table, whose width the host knows, not by the lengths, which
+// only the device does: a table far wider than its requests' caches pays for it.
 //
 // Measured: 256 caches of 4 heads, one token each past 1024, 16.6 us (a lane's
-// loads, four barriers and the launch; 43 us with keys read again for each digit);
-// 64 of up to 4096 cut to 2048 15 us and the move 35 (172 MB, 4.9 TB/s, a large
-// copy's rate).
+// loads, four barriers and the launch; 48 us with keys read again for each digit and
+// the move by itself) in tables of 1040 slots, 18 in 2048, 29 in 4096 and 8192 (a
+// selection of 1024 lanes of 8 keys for rows of 1025), 44 in 32,768 and 46 in 65,536
+// (keys read again); letting each row's length decide who moves it gained 0 to 2 us
+// there and cost others 1 to 3%.  64 of up to 4096 cut to 2048 15 us and the move 35
+// (172 MB, 4.9 TB/s, a large copy's rate).
 #include "attn_common.hpp"
 
 namespace eldr {
