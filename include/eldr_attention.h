@@ -23,7 +23,10 @@
  * hipStream_t passed as void*; the caller owns every buffer; calls are
  * asynchronous on `stream`, allocate nothing, keep no state, never
  * synchronise and can be captured in a graph; they return MOE_OK or a
- * negative MOE_ERR_* code (eldr_moe.h) before any launch.
+ * negative MOE_ERR_* code (eldr_moe.h) before any launch.  Queries, keys,
+ * values, outputs of attention, caches, rotation tables and the workspace are
+ * 16-byte aligned; every other array (lse, sinks, scales, accumulated weights,
+ * int32) 4-byte.
  *
  * The cache
  * ---------
@@ -32,8 +35,8 @@
  *
  *   b * block_stride + (h * block_size + o) * D
  *
- * (block_stride 0 stands for the dense Hkv * block_size * D; a larger one lets
- * keys and values, or layers, interleave in one allocation).  Offsets are
+ * (block_stride 0 stands for the dense Hkv * block_size * D; a larger one, a
+ * multiple of 16, lets keys and values, or layers, interleave in one allocation).  Offsets are
  * computed in 64 bits.  kv_type MOE_KV_BF16: values are bf16.  MOE_KV_FP8:
  * values are OCP e4m3 codes that stand for code * scale[h], with k_scale and
  * v_scale [Hkv] fp32 device arrays (NULL: all 1); ignored for bf16.
@@ -55,7 +58,8 @@
  * that, and in a group of one, each request reads its own row.  An empty
  * member's row is not read.)  group_start must not descend; it is taken
  * as clamped to [0, R], and requests outside every group share nothing.
- * n_groups = 0: nothing is shared and both pointers may be NULL.
+ * n_groups = 0: nothing is shared and both pointers may be NULL; more than
+ * MOE_ATTN_MAX_R is MOE_ERR_INVALID.
  */
 #ifndef ELDR_ATTENTION_H_
 #define ELDR_ATTENTION_H_
@@ -78,7 +82,7 @@ extern "C" {
 #define MOE_IN_FP32 1
 
 /* Limits.  D is 64, 128 or 256; Hkv divides Hq; block_size is a power of two. */
-#define MOE_ATTN_MAX_R 1024
+#define MOE_ATTN_MAX_R 1024 /* requests, and groups */
 #define MOE_ATTN_MAX_HEADS 256
 #define MOE_ATTN_MIN_BLOCK 16
 #define MOE_ATTN_MAX_BLOCK 1024
@@ -96,7 +100,8 @@ typedef struct moe_attn_dims {
 
 /*
  * moe_kv_append -- rotate the T new tokens' queries and keys by their
- * positions and store keys and values (d.R and d.max_blocks are not used).
+ * positions and store keys and values (d.R and d.max_blocks are checked as for
+ * the other calls, and not used).
  *
  *   for pair i < rot / 2 of token t, with a = pair_axis[i]:
  *     C = cos_table[positions[a, t], i], S = sin_table[positions[a, t], i]
@@ -203,7 +208,8 @@ int moe_attn_weights(const uint16_t* q, const void* k_cache, const int32_t* bloc
  * Order does not matter to attention without a window, whose keys carry their
  * positions, so nothing else has to move: one token over the budget costs one
  * row.  A row whose page is absent is not moved.  d.Hq and block_table as
- * above; 1 <= budget.
+ * above; 1 <= budget <= MOE_ATTN_MAX_TOKENS and R * Hkv <= 65535 (else
+ * MOE_ERR_UNSUPPORTED).
  */
 int moe_kv_evict(const float* weights, const int32_t* pos, const int32_t* lens,
                  const int32_t* seen, const int32_t* protect, const int32_t* block_table,

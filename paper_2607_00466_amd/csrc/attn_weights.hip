@@ -339,7 +339,7 @@ extern "C" int moe_attn_weights(const uint16_t* q, const void* k_cache, const in
   if (!q || !lens || !lse || !weights_out || !block_table || !k_cache ||
       (n_groups > 0 && (!group_start || !prefix_len)))
     return MOE_ERR_INVALID;
-  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(weights_in) || !aligned16(weights_out) ||
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned4(weights_in) || !aligned4(weights_out) ||
       !aligned4(block_table) || !aligned4(lens) || !aligned4(group_start) || !aligned4(prefix_len) ||
       !aligned4(k_scale) || !aligned4(lse))
     return MOE_ERR_UNSUPPORTED;

@@ -471,7 +471,7 @@ extern "C" int moe_kv_evict(const float* weights, const int32_t* pos, const int3
   if (d.max_blocks > 0 && (!weights || !pos || !block_table || !weights_out || !pos_out)) return MOE_ERR_INVALID;
   if (d.num_blocks > 0 && (!k_cache || !v_cache)) return MOE_ERR_INVALID;
   if (budget > MOE_ATTN_MAX_TOKENS || (int64_t)d.R * d.Hkv > 65535) return MOE_ERR_UNSUPPORTED;
-  if (!aligned16(weights) || !aligned16(weights_out) || !aligned16(k_cache) || !aligned16(v_cache) ||
+  if (!aligned4(weights) || !aligned4(weights_out) || !aligned16(k_cache) || !aligned16(v_cache) ||
       !aligned4(pos) || !aligned4(pos_out) || !aligned4(lens) || !aligned4(seen) || !aligned4(protect) ||
       !aligned4(block_table) || !aligned4(src) || !aligned4(new_lens))
     return MOE_ERR_UNSUPPORTED;
