@@ -41,12 +41,16 @@ class Heads:
 
 class Worker:
     """One layer's weights, and the batch's cache: `groups` equal groups of requests,
-    each behind `prefix` shared tokens and with `own` tokens of its own."""
+    each behind `prefix` shared tokens and with `own` tokens of its own, with room
+    for `steps` steps."""
 
     def __init__(self, shape: synth.LayerShape, heads: Heads, R: int, groups: int, prefix: int, own: int, budget: int,
                  steps: int, recent: int = 32, fp8: bool = False, seed: int = 0):
         if prefix % BLOCK or budget < prefix + recent:
             raise ValueError("the prefix is whole pages, and the budget holds it and the recent tokens")
+        if steps < 1 or own < 0 or groups < 1:
+            raise ValueError("a worker has a step to make, a group and no fewer than 0 tokens of its own a request")
+        self.left = steps
         self.shape, self.heads, self.budget, self.recent = shape, heads, budget, recent
         gen = torch.Generator(device="cuda").manual_seed(seed)
         normal = lambda *s, std=1.0: torch.empty(s, device="cuda").normal_(0, std, generator=gen)  # noqa: E731
@@ -123,6 +127,9 @@ class Worker:
 
     def attend(self, x):
         """Steps 1 to 3: the new tokens into the cache, and their attention."""
+        if self.left <= 0:
+            raise RuntimeError("the cache and the rotation tables have room for no further step")
+        self.left -= 1
         at = self.lens.long()
         self._append(x, self.seen, self._slots(self.rows, at), self.q)
         self.pos[self.rows, :, at] = self.seen[:, None]
@@ -170,8 +177,8 @@ def main(argv=None):
         y = w.step(x)
     end.record()
     torch.cuda.synchronize()
-    us = begin.elapsed_time(end) / max(1, a.steps - 1) * 1e3
-    print(f"{a.requests} requests, {a.groups} x {a.prefix} shared + {a.own} own tokens: {us:.1f} us a step; "
+    took = f"{begin.elapsed_time(end) / (a.steps - 1) * 1e3:.1f} us a step" if a.steps > 1 else "one step, not timed"
+    print(f"{a.requests} requests, {a.groups} x {a.prefix} shared + {a.own} own tokens: {took}; "
           f"union {int(w.moe.union_size.item())}, {int(w.lens[0].item())} tokens cached of {int(w.seen[0].item())} seen, "
           f"output {float(y.abs().mean()):.3f} mean |y|")
     return y
