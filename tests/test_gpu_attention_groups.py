@@ -1,4 +1,5 @@
-"""Groups that share a prefix, where the first members are empty."""
+"""Groups that share a prefix: where the first members are empty, and where pages inside
+the prefix are absent."""
 import numpy as np
 import pytest
 import torch
@@ -52,5 +53,20 @@ def test_a_prefix_is_read_through_the_first_member_that_holds_it(lens, group, ho
                 cache.table_np[r] = rng.integers(0, cache.nb, cache.max_blocks)
         cache.table.copy_(torch.from_numpy(cache.table_np))
     q = U.queries(len(lens), Hq, D)
+    _, lse = U.run_decode(cache, q, (group,))
+    _check_weights(cache, q, lse, (group,))
+
+
+@pytest.mark.parametrize("D,fp8,bs", [(128, False, 16), (64, True, 32), (256, False, 16)])
+def test_absent_pages_inside_a_prefix(D, fp8, bs):
+    G.say(f"case: holes in a shared prefix on both sides of slot 1024, D={D} fp8={fp8} bs={bs}")
+    lens, group = [2300, 2200, 2250, 2177], (0, 4, 2176)
+    cache = U.Cache(lens, 2, D, bs, fp8, seed=D, shared=(group,), max_blocks=2304 // bs)
+    # single pages, a whole 64-slot stage, pages on both sides of slot 1024, a run over slots 1920 to 2111
+    for lo, hi in ((0, 16), (80, 96), (320, 384), (1008, 1040), (1920, 2112)):
+        cache.table_np[0, lo // bs:-(-hi // bs)] = -1
+    cache.table_np[0, 700 // bs] = cache.nb + 3
+    cache.table.copy_(torch.from_numpy(cache.table_np))
+    q = U.queries(4, 16, D)
     _, lse = U.run_decode(cache, q, (group,))
     _check_weights(cache, q, lse, (group,))
