@@ -689,6 +689,12 @@ _KV_DTYPES = (torch.bfloat16, torch.float8_e4m3fn)
 _IN_TYPES = {torch.bfloat16: MOE_IN_BF16, torch.float32: MOE_IN_FP32}
 
 
+def _need_int32(value: int, name: str) -> None:
+    """ctypes would cut a larger count to its low 32 bits."""
+    if not -(1 << 31) <= value < 1 << 31:
+        raise ValueError(f"{name}: {value} is no 32-bit count")
+
+
 def attn_dims(R: int, Hq: int, Hkv: int, D: int, block_size: int, max_blocks: int, num_blocks: int,
               kv_dtype=torch.bfloat16, block_stride: int = 0) -> AttnDims:
     """The shape of one attention layer: R requests, Hq query heads over Hkv kv
@@ -696,6 +702,10 @@ def attn_dims(R: int, Hq: int, Hkv: int, D: int, block_size: int, max_blocks: in
     into num_blocks pages of kv_dtype."""
     if kv_dtype not in _KV_TYPES:
         raise ValueError(f"kv_dtype: expected torch.bfloat16 or torch.float8_e4m3fn, got {kv_dtype}")
+    if (R | Hq | Hkv | D | block_size | max_blocks | num_blocks) >> 31 > 0:
+        for name, value in zip(("R", "Hq", "Hkv", "D", "block_size", "max_blocks", "num_blocks"),
+                               (R, Hq, Hkv, D, block_size, max_blocks, num_blocks)):
+            _need_int32(value, name)
     return AttnDims(R, Hq, Hkv, D, block_size, max_blocks, num_blocks, _KV_TYPES[kv_dtype], block_stride)
 
 
@@ -810,6 +820,7 @@ def moe_attn_decode(q, k_cache, v_cache, block_table, lens, d: AttnDims, out, ls
     """Attention of one query token a request, q [R, Hq, D], over its cached tokens;
     out [R, Hq, D], lse [R, Hq] or None.  scale defaults to 1 / sqrt(D)."""
     n = d.R * d.Hq
+    _need_int32(window, "window")
     _need(q, "q", torch.bfloat16, n * d.D)
     _need(out, "out", torch.bfloat16, n * d.D)
     _need_opt(lse, "lse", torch.float32, n)
@@ -853,6 +864,8 @@ def moe_kv_evict(weights, pos, lens, seen, block_table, d: AttnDims, budget: int
     """Cut every request to its `budget` cached tokens of largest weight, in place
     (see include/eldr_attention.h for the order and for what moves)."""
     rows = d.R * d.Hkv * d.max_blocks * d.block_size
+    _need_int32(budget, "budget")
+    _need_int32(recent, "recent")
     _need(weights, "weights", torch.float32, rows)
     _need(pos, "pos", torch.int32, rows)
     _need(lens, "lens", torch.int32, d.R)
