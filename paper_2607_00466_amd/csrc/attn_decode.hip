@@ -16,9 +16,10 @@
 // are zipped by v_perm), a key tile handed over through LDS.  What bounds it is
 // HBM; the loads are non-temporal, so that they do not displace what the caches
 // hold (203 -> 178 us in the first case below).  Measured: 128 requests of up to
-// 8000 tokens (32 heads over 4 of 128, bf16, 1.1 GB) 177 us, 6.3 TB/s of a
-// streaming read's 7.05; 64 of 16384 in fp8 (1.1 GB) 166; D = 64 331 us and D = 256
-// 353 us for 2.1 GB.  Dealing the units to waves in place of workgroups (no merge
+// 8000 tokens (32 heads over 4 of 128, bf16, 1.1 GB) 178 to 181 us, 6.1 to 6.2 TB/s of
+// a streaming read's 7.05; 64 of 16384 in fp8 (1.1 GB) 167; D = 64 331 us and D = 256
+// 355 us for 2.1 GB.  Short segments are further off: 256 of up to 1500 in fp8 at D = 64
+// 48 us (208 MB, 61% of the read's rate).  Dealing the units to waves in place of workgroups (no merge
 // in LDS, four times the parts) measured 2 to 8% slower.
 //
 // The four waves of a workgroup take turns at a segment's 32-slot steps and
@@ -34,9 +35,17 @@ constexpr int kDecodeThreads = 256;
 constexpr int kDecodeWaves = kDecodeThreads / kWave;
 
 // Workgroups that share the own line.  More of them hide the ends of short
-// segments, fewer make longer segments and fewer parts.  Measured (us; 512, 768,
-// 1024): D = 128, 128 requests of up to 8000 178, 180, 182; 64 of up to 4000 51, 52,
-// 55; D = 64, 256 of up to 1500 in fp8 57, 50, 42.
+// segments, fewer make longer segments and fewer parts.  Measured (us, whole calls;
+// 512, 768, 1024):
+//   D = 64   256 of up to 1500 in fp8 67, 60, 57; in bf16 83, 87, 86
+//            128 of up to 8000 in fp8 113, 107, 110; in bf16 184, 189, 187
+//            64 of up to 700 21, 19, 19; 2 of 131,000 91, 94, 94
+//            256 of up to 1500 behind 8 x 2048 in fp8 105, 98, 94
+//   D = 128  128 of up to 8000 184, 186, 188; 256 of up to 1500 in fp8 86, 88, 87
+//            64 of up to 700 19, 18, 20
+//   D = 256  64 of up to 4000 63, 67, 71
+// So 1024 where rows are short: 10 to 17% for fp8 and for short contexts, against 2 to
+// 4% for long ones in bf16.
 constexpr int decode_wgs(int D) { return D == 64 ? 1024 : 512; }
 
 struct DecodeArgs {
@@ -388,8 +397,10 @@ int launch_decode(const DecodeArgs& a, const Pages& pg, float* ws, hipStream_t s
     hipLaunchKernelGGL((attn_shared_kernel<D, FP8>), dim3(kSharedWgs), dim3(kSharedThreads), S::kBytes + plan, s, sh, pg);
   }
   hipLaunchKernelGGL((attn_decode_kernel<D, FP8>), dim3(decode_wgs(D)), dim3(kDecodeThreads), lds, s, a, pg, parts);
-  // measured (us): 64 rows of 192 parts 8 by 256 threads and 31 by 64; 16,384 rows of
-  // about 10 parts 39 and 14
+  // measured (us, whole calls; 256 threads a row, 64): 64 rows of 131,000 slots 51, 59;
+  // 512 of 16,384 73, 74, and behind 8192 37, 43; 1024 of up to 8000 70, 69, and behind
+  // 8192 40, 42; 2048 of up to 8000 138, 136; 8192 behind 2048 73, 54; 16,384 of up to
+  // 1500 92, 71
   constexpr int64_t kFewRows = 1024;
   if (rows <= kFewRows)
     hipLaunchKernelGGL((attn_join_kernel<D, FP8, 256>), dim3((unsigned)rows), dim3(kDecodeThreads), 0, s, a, pg, parts, (int)rows);

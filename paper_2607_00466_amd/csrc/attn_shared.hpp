@@ -15,12 +15,13 @@
 // product costs: 64 behind 8192 48.8 -> 51.5 us, 64 behind 65536 127 -> 144, the
 // whole call; with one part these outputs' error was 1.3 times their rounding's.)
 //
-// Measured: 64 requests (32 heads over 4 of 128) against 8192 shared slots 25 us,
-// against 65536 113 us (610 TFLOP/s): a stage takes a workgroup 1.5 us, of which
-// its two waves a SIMD spend half in MFMAs and exponents and the rest in the
-// dependences between them; starting (plan, queries, first stage) takes 6 us and
-// handing over the parts 3.  Stages of 128 slots measured the same (4% faster at
-// D = 64), more stages in flight too.
+// Measured: 64 requests (32 heads over 4 of 128) against 8192 shared slots 28 us,
+// against 65536 132 to 146 us (470 to 520 TFLOP/s of the formula's products; a library
+// product 1400): a stage takes a workgroup 1.9 to 2.1 us.  (With one part 25 and 113 us,
+// 1.5 a stage, of which its two waves a SIMD spent half in MFMAs and exponents and the
+// rest in the dependences between them.)  Starting (plan, queries, first stage) takes
+// 6 us and handing over the parts 3.  Stages of 128 slots measured the same (4% faster
+// at D = 64), more stages in flight too.
 #pragma once
 
 #include "attn_plan.hpp"

@@ -13,8 +13,8 @@
 // tiles of its members' rows, dealt out as for moe_attn_decode.  A wave keeps its
 // rows' queries and lse in registers and takes 32 slots at a time, the next ones'
 // keys on their way.  Own slots are bound by HBM: keys once, weights in and out
-// (64 requests of up to 4000 tokens, 149 MB, 29.5 us, 5.0 TB/s; 64 of 16384 206 us,
-// 6.5 TB/s).  A prefix is bound by its steps: 64 requests behind 8192 slots take 26
+// (64 requests of up to 4000 tokens, 149 MB, 29 us, 5.1 TB/s; 64 of 16384, 1.11 GB,
+// 206 to 210 us, 5.3 TB/s, 75% of a streaming read).  A prefix is bound by its steps: 64 requests behind 8192 slots take 26
 // us where the bytes take 7; a step of 32 slots against 64 rows takes a wave 2.1 us,
 // 0.9 of them products, exponents and sums, and a workgroup has six after 5 us of
 // plan and rows (32 us while each of a tile's lse loads waited for the one before).

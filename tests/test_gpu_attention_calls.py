@@ -146,11 +146,16 @@ def test_weights_of_most_requests_and_groups(D, fp8):
         lens[s + 1] += n
     cache = U.Cache(lens, 1, D, 16, fp8, seed=D, shared=shared)
     q = U.queries(1024, 2, D)
-    _, lse = U.run_decode(cache, q, shared)
+    first, lse = U.run_decode(cache, q, shared)
     gs, pl, gs_np, pl_np = U.groups_of(shared, 1024)
     # as many groups as a call takes: the others are empty
     gs = torch.cat([gs, torch.full((1024 - pl.numel(),), 1024, dtype=torch.int32, device="cuda")])
     pl = torch.cat([pl, torch.zeros(1024 - pl.numel(), dtype=torch.int32, device="cuda")])
+    again, lse2 = torch.empty_like(first), torch.empty_like(lse)
+    d = cache.dims(2)
+    B.moe_attn_decode(q, cache.k, cache.v, cache.table, cache.lens, d, again, lse2, B.attn_workspace(d), gs, pl, cache.k_scale,
+                      cache.v_scale)
+    assert torch.equal(again, first) and torch.equal(lse2, lse)
     out = torch.full((1024, 1, cache.N), -2.0, device="cuda")
     want = A.weights(q.double().cpu().numpy(), cache.k_np, cache.table_np, cache.lens_np, lse.double().cpu().numpy(), D ** -0.5,
                      None, out.double().cpu().numpy(), gs_np, pl_np)
