@@ -144,14 +144,14 @@ int moe_kv_append(const void* q, const void* k, const void* v, int64_t q_stride,
  *
  * Query head h reads kv head h / (Hq / Hkv).  q, out [R, Hq, D] bf16; lse
  * [R, Hq] fp32 (NULL: not wanted); sinks [Hq] fp32 or NULL.  A request with no
- * visible slot gets out = 0 and lse = -inf, or the sink's value; a sink of -inf
- * weighs nothing.  A NaN that counts (in a query, a visible row or a sink) gives
- * NaN.  Where window > 0 no prefix is shared.  Scores, statistics and sums are
- * fp32; a weight enters the product with v in two bf16 parts, 16 bits of it, so
- * that out's error is that of its own rounding.  The result
- * does not depend on anything but the arguments' values (no atomics on floats);
- * how a long request is split depends on the whole batch's lengths, so a
- * request's last bits may differ between batches.
+ * visible slot, or none whose score is above -inf, gets out = 0 and lse = -inf,
+ * or the sink's value; a sink of -inf weighs nothing.  A NaN that counts (in a
+ * query, a visible row or a sink) gives NaN.  Where window > 0 no prefix is
+ * shared.  Scores, statistics and sums are fp32; a weight enters the product with
+ * v in two bf16 parts, 16 bits of it, so that out's error is that of its own
+ * rounding.  The result does not depend on anything but the arguments' values (no
+ * atomics on floats); how a long request is split depends on the whole batch's
+ * lengths, so a request's last bits may differ between batches.
  * ws: moe_attn_workspace_bytes(d) bytes, 16-byte aligned, whose contents mean
  * nothing between calls: one workspace serves every layer on a stream.
  */
