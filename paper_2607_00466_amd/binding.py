@@ -22,6 +22,7 @@ HEADER_PATH = os.path.join(INCLUDE_DIR, "eldr_moe.h")
 HEADER_PATHS = (HEADER_PATH, os.path.join(INCLUDE_DIR, "eldr_signature.h"),
                 os.path.join(INCLUDE_DIR, "eldr_calibration.h"),
                 os.path.join(INCLUDE_DIR, "eldr_attention.h"),
+                os.path.join(INCLUDE_DIR, "eldr_kv_cache.h"),
                 os.path.join(INCLUDE_DIR, "eldr_route.h"))
 
 MOE_OK = 0
@@ -102,6 +103,12 @@ _SIGNATURES = {
                         [_vp] * 3 + [ctypes.c_size_t, _vp]),
     "moe_attn_weights": (ctypes.c_int, [_vp] * 6 + [ctypes.c_int32, _vp, ctypes.c_float, _vp, AttnDims] + [_vp] * 3),
     "moe_kv_evict": (ctypes.c_int, [_vp] * 6 + [AttnDims, ctypes.c_int32, ctypes.c_int32] + [_vp] * 7),
+    "moe_kv_append_norm": (ctypes.c_int, [_vp] * 3 + [ctypes.c_int64] * 3 + [ctypes.c_int32] * 2 + [_vp, ctypes.c_int32] +
+                           [_vp] * 3 + [ctypes.c_int32] * 3 + [_vp, AttnDims, _vp, _vp, ctypes.c_float] + [_vp] * 6),
+    "moe_kv_append_int8": (ctypes.c_int, [_vp] * 3 + [ctypes.c_int64] * 3 + [ctypes.c_int32] * 2 + [_vp, ctypes.c_int32] +
+                           [_vp] * 3 + [ctypes.c_int32] * 3 + [_vp] * 3 + [AttnDims, _vp, _vp, ctypes.c_float] + [_vp] * 6),
+    "moe_kv_fork": (ctypes.c_int, [_vp] * 3 + [ctypes.c_int32, _vp, _vp, AttnDims, ctypes.c_int32, ctypes.c_int64] + [_vp] * 5),
+    "moe_kv_compact": (ctypes.c_int, [_vp] * 3 + [AttnDims, ctypes.c_int32, ctypes.c_int64] + [_vp] * 5),
     "moe_stream_read_probe": (ctypes.c_int, [_vp, ctypes.c_size_t, _vp, _vp]),
     "eldr_idf": (ctypes.c_int, [_vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _vp]),
     "eldr_signature": (ctypes.c_int, [_vp, _vp, ctypes.c_int32, ctypes.c_int32, _vp,
@@ -678,14 +685,15 @@ def moe_sig_request_counts(sig, block_table, n_blocks, out=None, stream=None) ->
 # ----------------------------------------------------------------------------- attention over the paged cache
 #
 # Caches are tensors whose first four dimensions are [num_blocks, Hkv,
-# block_size, D], of torch.bfloat16 or torch.float8_e4m3fn; only the block
-# stride may be larger than dense (d.block_stride), as where keys and values
-# interleave in one allocation.
+# block_size, D], of torch.bfloat16, torch.float8_e4m3fn (a scale a kv head) or
+# torch.int8 (a scale for each page and kv head); only the block stride may be
+# larger than dense (d.block_stride), as where keys and values interleave in one
+# allocation.
 
-MOE_KV_BF16, MOE_KV_FP8 = 0, 1
+MOE_KV_BF16, MOE_KV_FP8, MOE_KV_INT8 = 0, 1, 3
 MOE_IN_BF16, MOE_IN_FP32 = 0, 1
-_KV_TYPES = {torch.bfloat16: MOE_KV_BF16, torch.float8_e4m3fn: MOE_KV_FP8}
-_KV_DTYPES = (torch.bfloat16, torch.float8_e4m3fn)
+_KV_TYPES = {torch.bfloat16: MOE_KV_BF16, torch.float8_e4m3fn: MOE_KV_FP8, torch.int8: MOE_KV_INT8}
+_KV_DTYPES = {v: k for k, v in _KV_TYPES.items()}
 _IN_TYPES = {torch.bfloat16: MOE_IN_BF16, torch.float32: MOE_IN_FP32}
 
 
@@ -701,7 +709,7 @@ def attn_dims(R: int, Hq: int, Hkv: int, D: int, block_size: int, max_blocks: in
     heads of D values, pages of block_size slots, block tables [R, max_blocks]
     into num_blocks pages of kv_dtype."""
     if kv_dtype not in _KV_TYPES:
-        raise ValueError(f"kv_dtype: expected torch.bfloat16 or torch.float8_e4m3fn, got {kv_dtype}")
+        raise ValueError(f"kv_dtype: expected torch.bfloat16, torch.float8_e4m3fn or torch.int8, got {kv_dtype}")
     if (R | Hq | Hkv | D | block_size | max_blocks | num_blocks) >> 31 > 0:
         for name, value in zip(("R", "Hq", "Hkv", "D", "block_size", "max_blocks", "num_blocks"),
                                (R, Hq, Hkv, D, block_size, max_blocks, num_blocks)):
@@ -730,6 +738,24 @@ def _need_cache(t: torch.Tensor, name: str, d: AttnDims) -> None:
 def _need_opt(t, name: str, dtype: torch.dtype, numel: int) -> None:
     if t is not None:
         _need(t, name, dtype, numel)
+
+
+def _need_scales(k_scale, v_scale, d: AttnDims) -> None:
+    """One a kv head or none; of 8-bit integers, one for each page and kv head."""
+    if d.kv_type == MOE_KV_INT8:
+        if k_scale is None or v_scale is None:
+            raise ValueError("k_scale and v_scale: a cache of torch.int8 has both, [num_blocks, Hkv]")
+        _need(k_scale, "k_scale", torch.float32, d.num_blocks * d.Hkv)
+        _need(v_scale, "v_scale", torch.float32, d.num_blocks * d.Hkv)
+        return
+    _need_opt(k_scale, "k_scale", torch.float32, d.Hkv)
+    _need_opt(v_scale, "v_scale", torch.float32, d.Hkv)
+
+
+def _need_here(t: torch.Tensor, name: str) -> None:
+    """Kernels run on the current device."""
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: is on {t.device}, and the current device is cuda:{torch.cuda.current_device()}")
 
 
 def _need_rows(t: torch.Tensor, name: str, T: int, heads: int, D: int) -> int:
@@ -761,12 +787,9 @@ def _need_groups(group_start, prefix_len) -> int:
     return n
 
 
-def moe_kv_append(q, k, v, positions, pair_axis, cos, sin, slots, d: AttnDims, q_out, k_cache, v_cache,
-                  k_scale=None, v_scale=None, interleaved: bool = False, stream=None) -> None:
-    """Rotate q [T, Hq, D] into q_out and k [T, Hkv, D] by positions [n_axes, T], and
-    store k and v in the caches' slots.  q, k and v may be views of one projection's
-    rows; q and q_out may be None where only keys and values are wanted."""
-    T, Hq, Hkv, D = slots.numel(), d.Hq, d.Hkv, d.D
+def _append_rows(q, k, v, T: int, positions, pair_axis, cos, sin, d: AttnDims, q_out, interleaved: bool):
+    """What the appends' calls begin with: rows, their strides and type, T, rotation."""
+    Hq, Hkv, D = d.Hq, d.Hkv, d.D
     if positions.dim() != 2 or positions.shape[1] != T:
         raise ValueError(f"positions: expected [n_axes, {T}]")
     if cos.dim() != 2 or cos.shape != sin.shape:
@@ -790,19 +813,137 @@ def moe_kv_append(q, k, v, positions, pair_axis, cos, sin, slots, d: AttnDims, q
     _need(pair_axis, "pair_axis", i32, half)
     _need(cos, "cos", f32, max_pos * half)
     _need(sin, "sin", f32, max_pos * half)
-    _need(slots, "slots", i32, T)
-    if k_scale is not None:
-        _need(k_scale, "k_scale", f32, Hkv)
-    if v_scale is not None:
-        _need(v_scale, "v_scale", f32, Hkv)
+    return (pq, k.data_ptr(), v.data_ptr(), q_stride, k_stride, v_stride, _IN_TYPES[dtype], T, positions.data_ptr(), n_axes,
+            pair_axis.data_ptr(), cos.data_ptr(), sin.data_ptr(), max_pos, 2 * half, 1 if interleaved else 0), pq_out
+
+
+def moe_kv_append(q, k, v, positions, pair_axis, cos, sin, slots, d: AttnDims, q_out, k_cache, v_cache,
+                  k_scale=None, v_scale=None, interleaved: bool = False, stream=None) -> None:
+    """Rotate q [T, Hq, D] into q_out and k [T, Hkv, D] by positions [n_axes, T], and
+    store k and v in the caches' slots.  q, k and v may be views of one projection's
+    rows; q and q_out may be None where only keys and values are wanted."""
+    T = slots.numel()
+    rows, pq_out = _append_rows(q, k, v, T, positions, pair_axis, cos, sin, d, q_out, interleaved)
+    _need(slots, "slots", torch.int32, T)
+    _need_opt(k_scale, "k_scale", torch.float32, d.Hkv)
+    _need_opt(v_scale, "v_scale", torch.float32, d.Hkv)
     _need_cache(k_cache, "k_cache", d)
     _need_cache(v_cache, "v_cache", d)
-    status = load().moe_kv_append(
-        pq, k.data_ptr(), v.data_ptr(), q_stride, k_stride, v_stride, _IN_TYPES[dtype], T, positions.data_ptr(), n_axes,
-        pair_axis.data_ptr(), cos.data_ptr(), sin.data_ptr(), max_pos, 2 * half, 1 if interleaved else 0, slots.data_ptr(), d,
-        _ptr(k_scale), _ptr(v_scale), pq_out, k_cache.data_ptr(), v_cache.data_ptr(), _stream(stream))
+    status = load().moe_kv_append(*rows, slots.data_ptr(), d, _ptr(k_scale), _ptr(v_scale), pq_out, k_cache.data_ptr(),
+                                  v_cache.data_ptr(), _stream(stream))
     if status:
         _check("moe_kv_append", status)
+
+
+def moe_kv_append_norm(q, k, v, positions, pair_axis, cos, sin, slots, d: AttnDims, q_out, k_cache, v_cache, q_norm,
+                       k_norm, eps: float = 1e-6, k_scale=None, v_scale=None, interleaved: bool = False,
+                       stream=None) -> None:
+    """moe_kv_append, with each head of q and k first over the root of its mean square
+    and times q_norm, k_norm [D] fp32 (None: that side is not normed)."""
+    T = slots.numel()
+    rows, pq_out = _append_rows(q, k, v, T, positions, pair_axis, cos, sin, d, q_out, interleaved)
+    _need(slots, "slots", torch.int32, T)
+    _need_opt(q_norm, "q_norm", torch.float32, d.D)
+    _need_opt(k_norm, "k_norm", torch.float32, d.D)
+    _need_opt(k_scale, "k_scale", torch.float32, d.Hkv)
+    _need_opt(v_scale, "v_scale", torch.float32, d.Hkv)
+    _need_cache(k_cache, "k_cache", d)
+    _need_cache(v_cache, "v_cache", d)
+    _need_here(k_cache, "k_cache")
+    _check("moe_kv_append_norm", load().moe_kv_append_norm(
+        *rows, slots.data_ptr(), d, _ptr(q_norm), _ptr(k_norm), eps, _ptr(k_scale), _ptr(v_scale), pq_out, k_cache.data_ptr(),
+        v_cache.data_ptr(), _stream(stream)))
+
+
+def moe_kv_append_int8(q, k, v, positions, pair_axis, cos, sin, query_start, block_table, lens, d: AttnDims, q_out, k_cache,
+                       v_cache, k_scale, v_scale, q_norm=None, k_norm=None, eps: float = 1e-6, interleaved: bool = False,
+                       stream=None) -> None:
+    """New tokens into a cache of 8-bit integers: tokens query_start[r] ..
+    query_start[r + 1] - 1 go to request r's slots from lens[r] on (lens stays as it is);
+    k_scale, v_scale [num_blocks, Hkv] are brought up to date.  Norms as for
+    moe_kv_append_norm."""
+    T = k.shape[0]
+    rows, pq_out = _append_rows(q, k, v, T, positions, pair_axis, cos, sin, d, q_out, interleaved)
+    _need(query_start, "query_start", torch.int32, d.R + 1)
+    _need(block_table, "block_table", torch.int32, d.R * d.max_blocks)
+    _need(lens, "lens", torch.int32, d.R)
+    _need_opt(q_norm, "q_norm", torch.float32, d.D)
+    _need_opt(k_norm, "k_norm", torch.float32, d.D)
+    _need_cache(k_cache, "k_cache", d)
+    _need_cache(v_cache, "v_cache", d)
+    _need_scales(k_scale, v_scale, d)
+    _need_here(k_cache, "k_cache")
+    _check("moe_kv_append_int8", load().moe_kv_append_int8(
+        *rows, query_start.data_ptr(), block_table.data_ptr(), lens.data_ptr(), d, _ptr(q_norm), _ptr(k_norm), eps, pq_out,
+        k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), _stream(stream)))
+
+
+def _need_layers(k_cache, v_cache, k_scale, v_scale, d: AttnDims):
+    """The caches of one layer, or [layers, ...] of several: their count and stride."""
+    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name}: expected a torch tensor")
+        if t.dim() == 4:
+            _need_cache(t, name, d)
+        elif t.dim() != 5:
+            raise ValueError(f"{name}: expected [num_blocks, Hkv, block_size, D] or [layers, ...] of it, got {tuple(t.shape)}")
+    if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride():
+        raise ValueError("k_cache and v_cache: expected the same shape and strides")
+    layers, stride = 1, 0
+    if k_cache.dim() == 5:
+        layers, stride = k_cache.shape[0], k_cache.stride(0)
+        if layers > 0:
+            for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+                _need_cache_rows(t[0], name, d)
+        if layers == 1 or k_cache.numel() == 0:
+            stride = 0  # of no use
+    if d.kv_type == MOE_KV_INT8:
+        for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            _need(t, name, torch.float32, layers * d.num_blocks * d.Hkv)
+    _need_here(k_cache, "k_cache")
+    return layers, stride
+
+
+def _need_cache_rows(t: torch.Tensor, name: str, d: AttnDims) -> None:
+    """One layer's pages, of block stride d.block_stride (dense where that is 0)."""
+    if t.is_cuda and t.dtype is _KV_DTYPES[d.kv_type] and t.shape == (d.num_blocks, d.Hkv, d.block_size, d.D):
+        block = d.block_stride or d.Hkv * d.block_size * d.D
+        if t.numel() == 0 or (t.stride()[1:] == (d.block_size * d.D, d.D, 1) and (t.stride(0) == block or t.shape[0] == 1)):
+            return
+    _need_cache(t, name, d)
+
+
+def moe_kv_fork(parent, child, page, block_table, lens, d: AttnDims, k_cache, v_cache, k_scale=None, v_scale=None,
+                stream=None) -> None:
+    """Request child[i] becomes a copy of request parent[i] that shares its full pages;
+    what the parent's last page holds is copied to page[i], in every layer of the caches
+    [layers, num_blocks, Hkv, block_size, D] (or of one layer, without the first)."""
+    F = parent.numel()
+    i32 = torch.int32
+    _need(parent, "parent", i32, F)
+    _need(child, "child", i32, F)
+    _need(page, "page", i32, F)
+    _need(block_table, "block_table", i32, d.R * d.max_blocks)
+    _need(lens, "lens", i32, d.R)
+    layers, stride = _need_layers(k_cache, v_cache, k_scale, v_scale, d)
+    _check("moe_kv_fork", load().moe_kv_fork(
+        parent.data_ptr(), child.data_ptr(), page.data_ptr(), F, block_table.data_ptr(), lens.data_ptr(), d, layers, stride,
+        k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), _stream(stream)))
+
+
+def moe_kv_compact(remap, block_table, table_out, d: AttnDims, k_cache, v_cache, k_scale=None, v_scale=None,
+                   stream=None) -> None:
+    """Page b moves to page remap[b] (itself: it stays; negative: it is free) in every
+    layer; table_out (which may be block_table) is block_table with the pages' new
+    numbers, -1 for free ones."""
+    i32 = torch.int32
+    _need(remap, "remap", i32, d.num_blocks)
+    _need(block_table, "block_table", i32, d.R * d.max_blocks)
+    _need(table_out, "table_out", i32, d.R * d.max_blocks)
+    layers, stride = _need_layers(k_cache, v_cache, k_scale, v_scale, d)
+    _check("moe_kv_compact", load().moe_kv_compact(
+        remap.data_ptr(), block_table.data_ptr(), table_out.data_ptr(), d, layers, stride, k_cache.data_ptr(),
+        v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), _stream(stream)))
 
 
 def moe_attn_workspace_bytes(d: AttnDims) -> int:
@@ -829,8 +970,7 @@ def moe_attn_decode(q, k_cache, v_cache, block_table, lens, d: AttnDims, out, ls
     _need(block_table, "block_table", torch.int32, d.R * d.max_blocks)
     _need(lens, "lens", torch.int32, d.R)
     groups = _need_groups(group_start, prefix_len)
-    _need_opt(k_scale, "k_scale", torch.float32, d.Hkv)
-    _need_opt(v_scale, "v_scale", torch.float32, d.Hkv)
+    _need_scales(k_scale, v_scale, d)
     _need_opt(sinks, "sinks", torch.float32, d.Hq)
     ws_bytes = _need_ws(ws, d)
     _check("moe_attn_decode", load().moe_attn_decode(

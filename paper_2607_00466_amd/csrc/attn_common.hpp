@@ -76,7 +76,7 @@ inline int check_attn_dims(const moe_attn_dims& d) {
   if (d.R < 0 || d.Hq <= 0 || d.Hkv <= 0 || d.D <= 0 || d.block_size <= 0 || d.max_blocks < 0 ||
       d.num_blocks < 0 || d.block_stride < 0 || d.Hq % d.Hkv != 0)
     return MOE_ERR_INVALID;
-  if (d.kv_type != MOE_KV_BF16 && d.kv_type != MOE_KV_FP8) return MOE_ERR_INVALID;
+  if (d.kv_type != MOE_KV_BF16 && d.kv_type != MOE_KV_FP8 && d.kv_type != MOE_KV_INT8) return MOE_ERR_INVALID;
   const int64_t dense = (int64_t)d.Hkv * d.block_size * d.D;
   if (d.block_stride != 0 && d.block_stride < dense) return MOE_ERR_INVALID;
   if (d.R > MOE_ATTN_MAX_R || d.Hq > MOE_ATTN_MAX_HEADS) return MOE_ERR_UNSUPPORTED;

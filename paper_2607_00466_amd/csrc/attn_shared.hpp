@@ -44,6 +44,8 @@ struct SharedTile {
   static constexpr int kStageBytes = kStage * D * 2;      // of one cache
   static constexpr int kAhead = D == 256 ? 1 : 2;         // stages in flight
   static constexpr int kMergeWords = kQ * (D / 16 * 4 + 2);
+  // (pages of 8-bit integers) the scales of the two buffers' four tiles, keys' then values'
+  static constexpr int kScaleWords = 8;
   static constexpr int kBytes = 4 * kStageBytes > kRowWaves * kMergeWords * kWave * 4 ? 4 * kStageBytes
                                                                                       : kRowWaves * kMergeWords * kWave * 4;
   // Where piece c of row r lies: rows are rotated against each other so that 16
@@ -54,14 +56,17 @@ struct SharedTile {
   }
 };
 
+// LDS behind a stage's that holds its scales.
+constexpr int scale_bytes(int kv) { return kv == kKvInt8 ? 64 : 0; }
+
 // A thread's share of one stage of one cache, on its way from HBM to LDS.  Wave
 // w stages slots [8 w, 8 w + 8), half of a 16-slot tile, so all in one page:
 // pass i's piece is piece lane % kChunks of slot 8 w + lane / kChunks + i kRowsPass.
-template <int D, bool FP8>
+template <int D, int KV>
 struct Piece {
   using S = SharedTile<D>;
-  typedef typename std::conditional<FP8, u32x2, u32x4>::type Raw;
-  static constexpr int kElem = FP8 ? 1 : 2;
+  typedef typename std::conditional<is_byte(KV), u32x2, u32x4>::type Raw;
+  static constexpr int kElem = is_byte(KV) ? 1 : 2;
   static constexpr int kRowsPass = kWave / S::kChunks;
   Raw raw[S::kPieces];
   __device__ __forceinline__ void load(const char* tile, uint32_t off) {
@@ -73,8 +78,9 @@ struct Piece {
 #pragma unroll
     for (int i = 0; i < S::kPieces; ++i) {
       u32x4 x;
-      if constexpr (FP8)
-        x = u32x4{fp8_pair<false>(raw[i][0]), fp8_pair<true>(raw[i][0]), fp8_pair<false>(raw[i][1]), fp8_pair<true>(raw[i][1])};
+      if constexpr (is_byte(KV))
+        x = u32x4{byte_pair<KV, false>(raw[i][0]), byte_pair<KV, true>(raw[i][0]), byte_pair<KV, false>(raw[i][1]),
+                  byte_pair<KV, true>(raw[i][1])};
       else
         x = raw[i];
       // slots that do not count become zeros: their bits may be NaN
@@ -88,7 +94,7 @@ struct SharedArgs {
   const uint16_t* q;
   const char *k_cache, *v_cache;
   Groups gr;
-  const float* k_scale;
+  const float *k_scale, *v_scale;
   float *rows_part, *rest_part;  // [R * Hq][D + 4], [kSharedWgs][kRowsWg][D + 4]
   float scale;
   int32_t Hq, G;
@@ -101,16 +107,16 @@ struct SharedSegment {
   int first, table_row, rows, row0, h, k0, k1;
 };
 
-template <int D, bool FP8>
+template <int D, int KV>
 __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& pg, const SharedSegment& sg, char* lds,
                                               float* part, bool by_row) {
   using S = SharedTile<D>;
-  constexpr int kK = D / 32, kV = D / 16, kElem = FP8 ? 1 : 2;
+  constexpr int kK = D / 32, kV = D / 16, kElem = is_byte(KV) ? 1 : 2;
   const int lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int half = wave / kRowWaves, wave_row = sg.row0 + wave % kRowWaves * S::kQ * kRows;
   const bool live = wave_row < sg.rows;  // the wave has rows
-  const float unit = a.scale * kLog2e * (FP8 && a.k_scale ? a.k_scale[sg.h] : 1.0f);
+  const float unit = a.scale * kLog2e * (KV == kKvFp8 && a.k_scale ? a.k_scale[sg.h] : 1.0f);
   u32x4 q[S::kQ][kK];
 #pragma unroll
   for (int t = 0; t < S::kQ; ++t) {
@@ -134,12 +140,17 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
   }
   const int32_t* table = pg.table + (int64_t)sg.table_row * pg.max_blocks;
   // stage i on its way: set i % kAhead
-  Piece<D, FP8> next_k[S::kAhead], next_v[S::kAhead];
+  Piece<D, KV> next_k[S::kAhead], next_v[S::kAhead];
+  // of pages of 8-bit integers: an even wave's first lane has its tile's key scale, the
+  // second its value scale
+  float next_scale[S::kAhead];
+  const float* scales = KV == kKvInt8 ? (lane == 0 ? a.k_scale : a.v_scale) + sg.h : nullptr;
+  float* const scale_lds = reinterpret_cast<float*>(lds + S::kBytes);
   const int my_row = lane / S::kChunks;  // of the wave's eight, in pass 0
   const uint32_t off = (uint32_t)((wave % 2 * 8 + my_row) * D + lane % S::kChunks * 8) * kElem;
   uint32_t put[S::kPieces];
 #pragma unroll
-  for (int i = 0; i < S::kPieces; ++i) put[i] = S::at(wave * 8 + my_row + i * Piece<D, FP8>::kRowsPass, lane % S::kChunks);
+  for (int i = 0; i < S::kPieces; ++i) put[i] = S::at(wave * 8 + my_row + i * Piece<D, KV>::kRowsPass, lane % S::kChunks);
   // The pages of 64 16-slot tiles (a window), lane i the i-th's, asked for one
   // window ahead: a scalar load a stage would be waited for with every LDS read.
   // present[w % 2]: which tiles of window w count and have a page.
@@ -164,17 +175,23 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
     const int slot = k + wave / 2 * 16;
     int page = __builtin_amdgcn_readlane(pages, slot / 16 % kWave);
     page = pg.has(page) ? page : 0;
+    if constexpr (KV == kKvInt8) next_scale[set] = scales[(int64_t)page * pg.Hkv];
     const int64_t at = (page * pg.block_stride + (head_at + (slot & in_page)) * D) * kElem;
     next_k[set].load(a.k_cache + at, off);
     next_v[set].load(a.v_cache + at, off);
   };
   // stage k from its set to the buffer
-  const auto store = [&](int set, int k, char* to) {
+  const auto store = [&](int set, int k, char* to, float* scale_to) {
     const uint32_t there = tiles_there(k);
     const bool whole = there == 15u && k + kStage <= sg.k1;
     const int live = (there >> (wave / 2) & 1u) ? sg.k1 - (k + wave * 8 + my_row) : 0;
     next_k[set].store(to, put, whole, live);
     next_v[set].store(to + S::kStageBytes, put, whole, live);
+    if constexpr (KV == kKvInt8) {
+      // a tile without a slot that counts has no scale that counts
+      const bool any = (there >> (wave / 2) & 1u) && k + wave / 2 * 16 < sg.k1;
+      if (wave % 2 == 0 && lane < 2) scale_to[lane * 4 + wave / 2] = any ? next_scale[set] : 0.0f;
+    }
   };
   // where the lane's operands lie in a stage (the swizzle repeats every 16 rows)
   uint32_t k_at[kK], v_at[4];
@@ -188,10 +205,10 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
 #pragma unroll
   for (int i = 0; i < S::kAhead; ++i)
     if (sg.k0 + i * kStage < sg.k1) fetch(i, sg.k0 + i * kStage);
-  store(0, sg.k0, lds);
+  store(0, sg.k0, lds, scale_lds);
   __syncthreads();
   // one stage: k's slots lie in buffer `stage`; set (of k) is free again
-  const auto use = [&](int k, int set, int next_set, char* stage, char* other) {
+  const auto use = [&](int k, int set, int next_set, char* stage, char* other, const float* scale_at, float* scale_to) {
     if (k + S::kAhead * kStage < sg.k1) fetch(set, k + S::kAhead * kStage);
     const int k_mine = k + half * kStep;
     const uint32_t there = tiles_there(k) >> (2 * half);
@@ -210,10 +227,17 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
       }
       const bool whole = (there & 3u) == 3u && k_mine + kStep <= sg.k1;
       const auto keep = [&](int j) { return (there >> (j / 4) & 1u) && k_mine + (j / 4) * 16 + 4 * g + j % 4 < sg.k1; };
+      StepUnits<KV == kKvInt8> units;
+      if constexpr (KV == kKvInt8) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) units.score[b] = unit * scale_at[2 * half + b], units.value[b] = scale_at[4 + 2 * half + b];
+      } else {
+        units.score = unit;
+      }
       u32x4 most[S::kQ], rest[S::kQ];
 #pragma unroll
       for (int t = 0; t < S::kQ; ++t) {
-        const Weights p = softmax_step(s[t], unit, whole, keep, m[t], l[t], [&](float f) {
+        const Weights p = softmax_step(s[t], units, whole, keep, m[t], l[t], [&](float f) {
 #pragma unroll
           for (int c = 0; c < kV; ++c) acc[t][c] *= f;
         });
@@ -223,7 +247,7 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
       constexpr int kCols = kV < 8 ? kV : 8;
 #pragma unroll
       for (int w = 0; w < kV / kCols; ++w) {
-        Values<kCols * 16, false> v;
+        Values<kCols * 16, kKvBf16> v;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           // (neighbouring pieces of a row differ in the lowest bit of their place)
@@ -247,13 +271,13 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
         }
       }
     }
-    if (k + kStage < sg.k1) store(next_set, k + kStage, other);
+    if (k + kStage < sg.k1) store(next_set, k + kStage, other, scale_to);
     __syncthreads();
   };
   char* const buffers[2] = {lds, lds + 2 * S::kStageBytes};
   for (int k = sg.k0; k < sg.k1; k += 2 * kStage) {
-    use(k, 0, 1 % S::kAhead, buffers[0], buffers[1]);
-    if (k + kStage < sg.k1) use(k + kStage, 1 % S::kAhead, 0, buffers[1], buffers[0]);
+    use(k, 0, 1 % S::kAhead, buffers[0], buffers[1], scale_lds, scale_lds + S::kScaleWords);
+    if (k + kStage < sg.k1) use(k + kStage, 1 % S::kAhead, 0, buffers[1], buffers[0], scale_lds + S::kScaleWords, scale_lds);
   }
   // The halves add up: each hands the other the row tile that it does not finish
   // (tile t is finished by half t; with one tile the second half only hands over),
@@ -315,13 +339,13 @@ __device__ __forceinline__ void attend_shared(const SharedArgs& a, const Pages& 
   __syncthreads();
 }
 
-template <int D, bool FP8>
+template <int D, int KV>
 __global__ __launch_bounds__(kSharedThreads, 2) void attn_shared_kernel(SharedArgs a, Pages pg) {
   using S = SharedTile<D>;
   extern __shared__ char lds_shared[];
   __shared__ int waves[kSharedWaves];
   const int capacity = pg.capacity();
-  const Plan plan = make_plan<kSharedThreads>(a.gr, capacity, a.G, S::kRowsWg, reinterpret_cast<int*>(lds_shared + S::kBytes), waves);
+  const Plan plan = make_plan<kSharedThreads>(a.gr, capacity, a.G, S::kRowsWg, reinterpret_cast<int*>(lds_shared + S::kBytes + scale_bytes(KV)), waves);
   const int n = a.gr.n, row = plan.shared[n];
   const Deal deal(row * pg.Hkv, kSharedWgs);
   const int w = (int)blockIdx.x % kNumXcd * (kSharedWgs / kNumXcd) + (int)blockIdx.x / kNumXcd;
@@ -340,7 +364,7 @@ __global__ __launch_bounds__(kSharedThreads, 2) void attn_shared_kernel(SharedAr
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(sg) / 4); ++i) f[i] = __builtin_amdgcn_readfirstlane(f[i]);
     const bool begins = sg.k0 == 0;
-    attend_shared<D, FP8>(a, pg, sg, lds_shared,
+    attend_shared<D, KV>(a, pg, sg, lds_shared,
                           begins ? a.rows_part : a.rest_part + (int64_t)w * S::kRowsWg * (D + 4), begins);
     u += tiles;
   }

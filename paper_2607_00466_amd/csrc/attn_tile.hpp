@@ -12,22 +12,35 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-template <int D, bool FP8>
+// What a cache holds: the kernels' template argument.
+constexpr int kKvBf16 = 0, kKvFp8 = 1, kKvInt8 = 2;
+constexpr bool is_byte(int kv) { return kv != kKvBf16; }
+
+template <int D, int KV>
 struct Tile {
+  static constexpr bool kByte = is_byte(KV);
   static constexpr int kK = D / 32;       // MFMA steps of the first product
   static constexpr int kV = D / 16;       // value columns a lane holds
-  static constexpr int kElem = FP8 ? 1 : 2;
+  static constexpr int kElem = kByte ? 1 : 2;
 
   // Value index of the first of the 8 that a lane holds for step s.
   static __device__ __forceinline__ int q_at(int s, int g) {
-    return FP8 ? (s / 2) * 64 + g * 16 + (s % 2) * 8 : s * 32 + g * 8;
+    return kByte ? (s / 2) * 64 + g * 16 + (s % 2) * 8 : s * 32 + g * 8;
   }
 };
 
-// Two fp8 codes (bytes 0, 1 or 2, 3 of w) as bf16: exact.
-template <bool HI>
-__device__ __forceinline__ uint32_t fp8_pair(uint32_t w) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
+// Two codes as bf16, in one word: exact.  A whole number of 8 bits has no bits past
+// the upper half of its fp32.
+__device__ __forceinline__ uint32_t int8_pair(int a, int b) {
+  return __builtin_amdgcn_perm(__float_as_uint((float)b), __float_as_uint((float)a), 0x07060302u);
+}
+__device__ __forceinline__ int byte_of(uint32_t w, int i) { return (int8_t)(w >> (8 * i)); }
+
+// The codes in bytes 0, 1 or 2, 3 of w.
+template <int KV, bool HI>
+__device__ __forceinline__ uint32_t byte_pair(uint32_t w) {
+  if constexpr (KV == kKvFp8) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
+  else return int8_pair(byte_of(w, HI ? 2 : 0), byte_of(w, HI ? 3 : 1));
 }
 
 // v, or zeros: a mask, so that the load that gave v stays where it is (a select
@@ -56,10 +69,10 @@ __device__ __forceinline__ V tile_load(const char* p) {
 }
 
 // One 16-slot tile of keys as MFMA operands.
-template <int D, bool FP8>
+template <int D, int KV>
 struct Keys {
-  using T = Tile<D, FP8>;
-  static constexpr int kLoads = FP8 ? T::kK / 2 : T::kK;
+  using T = Tile<D, KV>;
+  static constexpr int kLoads = T::kByte ? T::kK / 2 : T::kK;
   u32x4 raw[kLoads];
   template <bool STREAM>
   __device__ __forceinline__ void load(const char* rows, int n, int g) {
@@ -67,10 +80,10 @@ struct Keys {
     for (int i = 0; i < kLoads; ++i) raw[i] = tile_load<STREAM, u32x4>(rows + (uint32_t)(n * D * T::kElem + i * 64 + g * 16));
   }
   __device__ __forceinline__ u32x4 operand(int s) const {
-    if constexpr (FP8) {
+    if constexpr (T::kByte) {
       const u32x4 r = raw[s / 2];
       const uint32_t a = r[(s % 2) * 2], b = r[(s % 2) * 2 + 1];
-      return u32x4{fp8_pair<false>(a), fp8_pair<true>(a), fp8_pair<false>(b), fp8_pair<true>(b)};
+      return u32x4{byte_pair<KV, false>(a), byte_pair<KV, true>(a), byte_pair<KV, false>(b), byte_pair<KV, true>(b)};
     } else {
       return raw[s];
     }
@@ -82,9 +95,9 @@ struct Keys {
 // own load touches 64 pieces of 16 rows), and takes the operands from a stretch
 // of LDS of its own, whose rows are rotated against each other to spread them
 // over the banks.  No barrier of the workgroup: the stretch is one wave's.
-template <int D, bool FP8>
+template <int D, int KV>
 struct StagedKeys {
-  using T = Tile<D, FP8>;
+  using T = Tile<D, KV>;
   static constexpr int kRowBytes = D * T::kElem, kChunks = kRowBytes / 16;
   static constexpr int kTileBytes = 16 * kRowBytes, kLoads = kTileBytes / (16 * kWave);
   static constexpr int kBytes = 2 * kTileBytes;  // of LDS, a wave
@@ -119,9 +132,9 @@ struct StagedKeys {
 
 // 32 slots of values: the lane's kV columns of its 8 slots, 4 of each 16-slot
 // tile (rows 4 g .. 4 g + 3).
-template <int D, bool FP8>
+template <int D, int KV>
 struct Values {
-  using T = Tile<D, FP8>;
+  using T = Tile<D, KV>;
   static constexpr int kBytes = T::kV * T::kElem;  // a slot's, 4 to 32
   static constexpr int kWords = kBytes / 4;
   uint32_t raw[8][kWords];
@@ -155,11 +168,13 @@ struct Values {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t *a = raw[2 * i], *b = raw[2 * i + 1];
-      if constexpr (FP8) {
+      if constexpr (KV == kKvInt8) {
+        v[i] = int8_pair(byte_of(a[c / 4], c % 4), byte_of(b[c / 4], c % 4));
+      } else if constexpr (KV == kKvFp8) {
         // the pair's bytes side by side, then both to bf16
         const uint32_t sel = (c & 2) ? 0x07030602u : 0x05010400u;
         const uint32_t z = __builtin_amdgcn_perm(b[c / 4], a[c / 4], sel);
-        v[i] = (c & 1) ? fp8_pair<true>(z) : fp8_pair<false>(z);
+        v[i] = (c & 1) ? byte_pair<KV, true>(z) : byte_pair<KV, false>(z);
       } else {
         v[i] = __builtin_amdgcn_perm(b[c / 2], a[c / 2], (c & 1) ? 0x07060302u : 0x05040100u);
       }
@@ -199,13 +214,26 @@ struct Weights {
   }
 };
 
+// What scales a step's two 16-slot tiles: their scores (in base-2 units), and,
+// where VALUES, their weights in the product with the values.
+template <bool VALUES>
+struct StepUnits {
+  float score[2], value[2];
+  __device__ __forceinline__ float of_score(int j) const { return score[j / 4]; }
+};
+template <>
+struct StepUnits<false> {
+  float score;
+  __device__ __forceinline__ float of_score(int) const { return score; }
+};
+
 // One step of the softmax of query row lane % 16 over the lane's 8 of 32 slots:
 // the weights exp2(unit s - m) as the second product's operands.  m: the row's
 // reference (-inf before the first slot that counts); l: this lane's part of the
 // sum, of the weights in 32 bits; keep(j): slot j counts (asked unless `whole`);
 // rescale(f): called, for all lanes, when the sums so far become f times as much.
-template <typename Keep, typename Rescale>
-__device__ __forceinline__ Weights softmax_step(const f32x4 (&s)[2], float unit, bool whole, Keep keep, float& m, float& l,
+template <bool VALUES, typename Keep, typename Rescale>
+__device__ __forceinline__ Weights softmax_step(const f32x4 (&s)[2], const StepUnits<VALUES>& unit, bool whole, Keep keep, float& m, float& l,
                                               Rescale rescale) {
   float e[8];
   // the largest in the branch that makes the exponents: after a merge the
@@ -213,7 +241,7 @@ __device__ __forceinline__ Weights softmax_step(const f32x4 (&s)[2], float unit,
   const auto largest = [&] { return fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(e[0], e[1]), e[2]), e[3]), e[4]), e[5]), e[6]), e[7]); };
   const auto exponents = [&](float base) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = fmaf(s[j / 4][j % 4], unit, -base);
+    for (int j = 0; j < 8; ++j) e[j] = fmaf(s[j / 4][j % 4], unit.of_score(j), -base);
     if (whole) return largest();
 #pragma unroll
     for (int j = 0; j < 8; ++j) e[j] = keep(j) ? e[j] : -INFINITY;
@@ -234,6 +262,7 @@ __device__ __forceinline__ Weights softmax_step(const f32x4 (&s)[2], float unit,
   for (int j = 0; j < 8; ++j) {
     e[j] = exp2_fast(e[j]);
     l += e[j];
+    if constexpr (VALUES) e[j] *= unit.value[j / 4];
   }
   return Weights(e);
 }

@@ -51,7 +51,7 @@ struct Span {
 
 // A 16-row tile's queries and lse (in base-2 units): row 16 t + lane % 16 as the
 // operand, rows 4 (lane / 16) + i as results.
-template <int D, bool FP8>
+template <int D, int KV>
 __device__ __forceinline__ void load_rows(const WeightArgs& a, const Span& sp, int row0, u32x4 (&q)[D / 32], f32x4& lse) {
   const int lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
   const auto request = [&](int row) { return sp.first + (a.pad <= kRows ? row >> a.pad_shift : row / a.pad); };
@@ -60,7 +60,7 @@ __device__ __forceinline__ void load_rows(const WeightArgs& a, const Span& sp, i
     const int req = request(row0 + n), i = head(row0 + n);
     const uint16_t* src = a.q + ((int64_t)min(req, sp.end - 1) * a.Hq + sp.h * a.G + (i < a.G ? i : 0)) * D;
 #pragma unroll
-    for (int s = 0; s < D / 32; ++s) q[s] = *reinterpret_cast<const u32x4*>(src + Tile<D, FP8>::q_at(s, g));
+    for (int s = 0; s < D / 32; ++s) q[s] = *reinterpret_cast<const u32x4*>(src + Tile<D, KV>::q_at(s, g));
   }
   // (what does not count is set by bits: a select would put each load behind a branch, one wait after another)
 #pragma unroll
@@ -94,16 +94,16 @@ __device__ __forceinline__ void sum_heads(f32x4& x, int in_tile) {
 
 // The tiles of rows from sp.row0 on, of requests of up to 16 rows; a lane has up
 // to PER requests in a tile, every 4 / PER-th of its rows.
-template <int D, bool FP8, int TILES, int PER>
+template <int D, int KV, int TILES, int PER>
 __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, const Span& sp, const int* group,
                                       char* stage) {
-  using T = Tile<D, FP8>;
+  using T = Tile<D, KV>;
   const int lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const float unit = a.scale * kLog2e * (FP8 && a.k_scale ? a.k_scale[sp.h] : 1.0f);
+  const float unit = a.scale * kLog2e * (KV == kKvFp8 && a.k_scale ? a.k_scale[sp.h] : 1.0f);
   const int32_t* table = pg.table + (int64_t)sp.table_row * pg.max_blocks;
   const int64_t N = pg.capacity();
-  char* mine_lds = stage + wave * StagedKeys<D, FP8>::kBytes;
+  char* mine_lds = stage + wave * StagedKeys<D, KV>::kBytes;
   constexpr int kEach = 4 / PER;
   const int64_t next_request = (int64_t)pg.Hkv * N;
   u32x4 q[TILES][T::kK];
@@ -114,7 +114,7 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
 #pragma unroll
   for (int t = 0; t < TILES; ++t) {
     const int row0 = sp.row0 + t * kRows;
-    load_rows<D, FP8>(a, sp, row0, q[t], lse[t]);
+    load_rows<D, KV>(a, sp, row0, q[t], lse[t]);
     // (kept within the span's requests, so that what it names can always be read)
     const int first = min(sp.first + ((row0 + 4 * g) >> a.pad_shift), sp.end - 1);
     at[t] = ((int64_t)first * pg.Hkv + sp.h) * N;
@@ -129,7 +129,7 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
   constexpr int kAhead = TILES == 1 && D != 256 ? 2 : 1;
   constexpr int kStride = kWeightWaves * kStep;
   struct Set {
-    StagedKeys<D, FP8> keys;
+    StagedKeys<D, KV> keys;
     float before[TILES][2][PER];
     StepPages pages;
   } sets[kAhead];
@@ -155,12 +155,12 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
   };
   const auto use = [&](Set& st, int k) {
     float sum[TILES][2][PER];
-    Keys<D, FP8> keys[2];
+    Keys<D, KV> keys[2];
     st.keys.put(mine_lds);
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int i = 0; i < Keys<D, FP8>::kLoads; ++i) keys[b].raw[i] = StagedKeys<D, FP8>::get(mine_lds, b, i, n, g);
+      for (int i = 0; i < Keys<D, KV>::kLoads; ++i) keys[b].raw[i] = StagedKeys<D, KV>::get(mine_lds, b, i, n, g);
     // the set is free: the step kAhead on is asked for before this one is computed
     const bool there[2] = {pg.has(st.pages.b0), pg.has(st.pages.b1)};
     float before[TILES][2][PER];
@@ -225,18 +225,18 @@ __device__ __forceinline__ void weigh(const WeightArgs& a, const Pages& pg, cons
 
 // The same for requests of more than 16 rows: tile by tile of one request, the
 // queries read again for every step.
-template <int D, bool FP8>
+template <int D, int KV>
 __device__ __forceinline__ void weigh_wide(const WeightArgs& a, const Pages& pg, const Span& sp, const int* group) {
-  using T = Tile<D, FP8>;
+  using T = Tile<D, KV>;
   const int lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const float unit = a.scale * kLog2e * (FP8 && a.k_scale ? a.k_scale[sp.h] : 1.0f);
+  const float unit = a.scale * kLog2e * (KV == kKvFp8 && a.k_scale ? a.k_scale[sp.h] : 1.0f);
   const int32_t* table = pg.table + (int64_t)sp.table_row * pg.max_blocks;
   const int64_t N = pg.capacity();
   for (int k = sp.k0 / kStep * kStep + wave * kStep; k < sp.k1; k += kWeightWaves * kStep) {
     const StepPages pages = step_pages(pg, table, k);
     const bool there[2] = {pg.has(pages.b0), pg.has(pages.b1)};
-    Keys<D, FP8> keys[2];
+    Keys<D, KV> keys[2];
     keys[0].template load<false>(a.k_cache + pg.row(there[0] ? pages.b0 : 0, sp.h, k) * T::kElem, n, g);
     keys[1].template load<false>(a.k_cache + pg.row(there[1] ? pages.b1 : 0, sp.h, k + 16) * T::kElem, n, g);
     for (int row0 = sp.row0; row0 < sp.row1; row0 += a.pad) {
@@ -246,7 +246,7 @@ __device__ __forceinline__ void weigh_wide(const WeightArgs& a, const Pages& pg,
       for (int part = 0; part < a.pad; part += kRows) {
         u32x4 q[T::kK];
         f32x4 lse;
-        load_rows<D, FP8>(a, sp, row0 + part, q, lse);
+        load_rows<D, KV>(a, sp, row0 + part, q, lse);
         f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (int i = 0; i < T::kK; ++i) {
@@ -269,11 +269,11 @@ __device__ __forceinline__ void weigh_wide(const WeightArgs& a, const Pages& pg,
   }
 }
 
-template <int D, bool FP8>
+template <int D, int KV>
 __global__ __launch_bounds__(kWeightThreads, 2) void attn_weights_kernel(WeightArgs a, Pages pg, int member_rows) {
   extern __shared__ int lds[];
   __shared__ int waves[kWeightWaves];
-  __shared__ __attribute__((aligned(16))) char stage[kWeightWaves * StagedKeys<D, FP8>::kBytes];
+  __shared__ __attribute__((aligned(16))) char stage[kWeightWaves * StagedKeys<D, KV>::kBytes];
   const int capacity = pg.capacity();
   const Plan plan = make_plan<kWeightThreads>(a.gr, capacity, a.pad, member_rows, lds, waves);
   const int R = a.gr.R, n = a.gr.n, wgs = gridDim.x;
@@ -307,19 +307,19 @@ __global__ __launch_bounds__(kWeightThreads, 2) void attn_weights_kernel(WeightA
     int* f = reinterpret_cast<int*>(&sp);
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(sp) / 4); ++i) f[i] = __builtin_amdgcn_readfirstlane(f[i]);
-    if (a.pad > kRows) weigh_wide<D, FP8>(a, pg, sp, plan.group);
-    else if (sp.group < 0) weigh<D, FP8, 1, 1>(a, pg, sp, plan.group, stage);
-    else if (a.pad == 1) weigh<D, FP8, member_tiles(D, 1), 4>(a, pg, sp, plan.group, stage);
-    else if (a.pad == 2) weigh<D, FP8, member_tiles(D, 2), 2>(a, pg, sp, plan.group, stage);
-    else weigh<D, FP8, member_tiles(D, 4), 1>(a, pg, sp, plan.group, stage);
+    if (a.pad > kRows) weigh_wide<D, KV>(a, pg, sp, plan.group);
+    else if (sp.group < 0) weigh<D, KV, 1, 1>(a, pg, sp, plan.group, stage);
+    else if (a.pad == 1) weigh<D, KV, member_tiles(D, 1), 4>(a, pg, sp, plan.group, stage);
+    else if (a.pad == 2) weigh<D, KV, member_tiles(D, 2), 2>(a, pg, sp, plan.group, stage);
+    else weigh<D, KV, member_tiles(D, 4), 1>(a, pg, sp, plan.group, stage);
     u += __builtin_amdgcn_readfirstlane(tiles);
   }
 }
 
-template <int D, bool FP8>
+template <int D, int KV>
 int launch_weights(const WeightArgs& a, const Pages& pg, hipStream_t s) {
   const int member_rows = a.pad > kRows ? a.pad : member_tiles(D, a.pad) * kRows;
-  hipLaunchKernelGGL((attn_weights_kernel<D, FP8>), dim3(kWeightWgs), dim3(kWeightThreads), Plan::bytes(a.gr.R, a.gr.n), s, a,
+  hipLaunchKernelGGL((attn_weights_kernel<D, KV>), dim3(kWeightWgs), dim3(kWeightThreads), Plan::bytes(a.gr.R, a.gr.n), s, a,
                      pg, member_rows);
   return eldr_host::launch_status();
 }
@@ -334,6 +334,7 @@ extern "C" int moe_attn_weights(const uint16_t* q, const void* k_cache, const in
   using namespace eldr_host;
   int st = check_attn_dims(d);
   if (st != MOE_OK) return st;
+  if (d.kv_type == MOE_KV_INT8) return MOE_ERR_UNSUPPORTED;  // (what weights lead to, eviction, does not know pages with scales of their own)
   if (n_groups < 0 || n_groups > MOE_ATTN_MAX_R || !(scale == scale)) return MOE_ERR_INVALID;
   if (d.R == 0 || d.max_blocks == 0 || d.num_blocks == 0) return MOE_OK;
   if (!q || !lens || !lse || !weights_out || !block_table || !k_cache ||
@@ -355,7 +356,7 @@ extern "C" int moe_attn_weights(const uint16_t* q, const void* k_cache, const in
   const eldr::Pages pg = pages_of(d, block_table);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const bool fp8 = d.kv_type == MOE_KV_FP8;
-  if (d.D == 64) return fp8 ? eldr::launch_weights<64, true>(a, pg, s) : eldr::launch_weights<64, false>(a, pg, s);
-  if (d.D == 128) return fp8 ? eldr::launch_weights<128, true>(a, pg, s) : eldr::launch_weights<128, false>(a, pg, s);
-  return fp8 ? eldr::launch_weights<256, true>(a, pg, s) : eldr::launch_weights<256, false>(a, pg, s);
+  if (d.D == 64) return fp8 ? eldr::launch_weights<64, eldr::kKvFp8>(a, pg, s) : eldr::launch_weights<64, eldr::kKvBf16>(a, pg, s);
+  if (d.D == 128) return fp8 ? eldr::launch_weights<128, eldr::kKvFp8>(a, pg, s) : eldr::launch_weights<128, eldr::kKvBf16>(a, pg, s);
+  return fp8 ? eldr::launch_weights<256, eldr::kKvFp8>(a, pg, s) : eldr::launch_weights<256, eldr::kKvBf16>(a, pg, s);
 }

@@ -465,6 +465,7 @@ extern "C" int moe_kv_evict(const float* weights, const int32_t* pos, const int3
   using namespace eldr_host;
   int st = check_attn_dims(d);
   if (st != MOE_OK) return st;
+  if (d.kv_type == MOE_KV_INT8) return MOE_ERR_UNSUPPORTED;  // (a moved row would need its new page's scale)
   if (budget < 1 || recent < 0) return MOE_ERR_INVALID;
   if (d.R == 0) return MOE_OK;
   if (!lens || !seen || !src || !new_lens || new_lens == lens) return MOE_ERR_INVALID;

@@ -1,0 +1,159 @@
+"""moe_kv_append_norm against the oracle: bit for bit where fp32 says what the bits are,
+and within derived bounds of the formula in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_00466_amd import binding as B
+from tests.kv_cache_util import FP8, Rows, bits, dev, i32
+
+pytestmark = pytest.mark.gpu
+
+EDGE = pytest.mark.parametrize("T,Hq,Hkv,D,rot,bs", [
+    (1, 8, 2, 128, 128, 16), (5, 4, 4, 64, 64, 16), (37, 12, 3, 64, 32, 32), (16, 16, 2, 256, 256, 16), (3, 71, 1, 128, 16, 64),
+    (130, 6, 2, 256, 64, 16), (9, 4, 1, 128, 0, 16)])
+
+
+def call(r, bs, fp8=False, eps=1e-6, slots=None, q=True, norms=(True, True), fn=B.moe_kv_append_norm, k_scale=None, v_scale=None):
+    nb = -(-r.T // bs) + 2
+    if slots is None:
+        slots = np.random.default_rng(3).permutation(nb * bs)[:r.T]
+    d = B.attn_dims(0, r.Hq, r.Hkv, r.D, bs, 1, nb, FP8 if fp8 else torch.bfloat16)
+    k, v = (torch.full((nb, r.Hkv, bs, r.D), 3.0, device="cuda").to(FP8 if fp8 else torch.bfloat16) for _ in "kv")
+    args = [r.q if q else None, r.k, r.v, r.positions, r.axis, r.cos, r.sin, i32(slots), d, r.q_out if q else None, k, v]
+    kw = dict(k_scale=k_scale, v_scale=v_scale, interleaved=r.interleaved)
+    if fn is B.moe_kv_append_norm:
+        args += [r.q_norm if norms[0] else None, r.k_norm if norms[1] else None]
+        kw["eps"] = eps
+    fn(*args, **kw)
+    torch.cuda.synchronize()
+    return k, v, slots
+
+
+def stored(x, scale, fp8):
+    """fp32 rows [T, Hkv, D] as the cache holds them."""
+    t = torch.from_numpy(np.ascontiguousarray(x, np.float32))
+    if not fp8:
+        return t.bfloat16()
+    t = t / (1.0 if scale is None else scale.cpu()[:, None])
+    return t.clamp(-448, 448).to(FP8)
+
+
+@EDGE
+@pytest.mark.parametrize("fp32,fp8,interleaved,axes", [(True, False, False, 1), (False, True, True, 3), (False, False, True, 1),
+                                                       (True, True, False, 2)])
+def test_bits(T, Hq, Hkv, D, rot, bs, fp32, fp8, interleaved, axes):
+    r = Rows(T, Hq, Hkv, D, rot, fp32=fp32, axes=axes, interleaved=interleaved, seed=T + D)
+    scales = [dev(np.random.default_rng(i).uniform(0.01, 0.1, Hkv).astype(np.float32)) if fp8 else None for i in range(2)]
+    k, v, slots = call(r, bs, fp8, k_scale=scales[0], v_scale=scales[1])
+    want = torch.from_numpy(r.expected("q")).bfloat16()
+    assert torch.equal(bits(r.q_out.cpu()), bits(want))
+    for cache, x, s in ((k, r.expected("k"), scales[0]), (v, r.numpy("v"), scales[1])):
+        rows = cache.cpu()
+        got = torch.stack([bits(rows)[s // bs, :, s % bs] for s in slots])
+        assert torch.equal(got, bits(stored(x, s, fp8)))
+        rest = torch.ones(rows.shape[0] * bs, dtype=torch.bool)
+        rest[torch.from_numpy(np.asarray(slots))] = False
+        assert (rows.float().permute(0, 2, 1, 3).reshape(-1, Hkv, D)[rest] == 3.0).all()  # nothing else was written
+
+
+@EDGE
+def test_against_64_bits(T, Hq, Hkv, D, rot, bs):
+    """bf16's half step 2^-8, and before it: the root's rounding, two products (2^-24
+    each) and a rotation of two products and a sum (3 of 2^-24 of the pair's larger sum)."""
+    r = Rows(T, Hq, Hkv, D, rot, seed=1)
+    call(r, bs)
+    want = r.expected("q", exact=True)
+    pair = np.abs(want) + np.linalg.norm(want, axis=-1, keepdims=True)
+    tol = 2.0 ** -8 * np.abs(want) + 6 * 2.0 ** -24 * pair * 1.01 + 1e-38
+    assert (np.abs(r.q_out.double().cpu().numpy() - want) <= tol * 1.01).all()
+
+
+def test_without_norms_it_is_moe_kv_append():
+    for fp8 in (False, True):
+        a, b = (Rows(33, 8, 2, 128, 64, fp32=False, axes=2, seed=4) for _ in "ab")
+        ka, va, _ = call(a, 16, fp8, norms=(False, False))
+        kb, vb, _ = call(b, 16, fp8, fn=B.moe_kv_append)
+        assert torch.equal(bits(ka), bits(kb)) and torch.equal(bits(va), bits(vb)) and torch.equal(bits(a.q_out), bits(b.q_out))
+
+
+@pytest.mark.parametrize("norms", [(True, False), (False, True)])
+def test_one_side_normed(norms):
+    r = Rows(21, 4, 2, 64, 64, seed=5)
+    k, _, slots = call(r, 16, norms=norms)
+    r.qn_np, r.kn_np = (w if on else None for w, on in zip((r.qn_np, r.kn_np), norms))
+    assert torch.equal(bits(r.q_out.cpu()), bits(torch.from_numpy(r.expected("q")).bfloat16()))
+    got = torch.stack([bits(k.cpu())[s // 16, :, s % 16] for s in slots])
+    assert torch.equal(got, bits(torch.from_numpy(r.expected("k")).bfloat16()))
+
+
+def test_keys_alone_absent_slots_and_absent_positions():
+    r = Rows(7, 4, 2, 128, 128, seed=6)
+    r.positions[0, 2] = 97  # past the tables
+    r.positions_np[0, 2] = 97
+    slots = [5, -1, 6, 10 ** 6, 0, 17, 31]
+    k, v, _ = call(r, 16, slots=slots, q=False)
+    assert (r.q_out == 7).all()
+    want, rows = torch.from_numpy(r.expected("k")).bfloat16(), k.cpu()
+    for t, s in enumerate(slots):
+        if 0 <= s < 48:
+            got = rows[s // 16, :, s % 16]
+            assert torch.equal(got.isnan(), want[t].isnan()) and torch.equal(bits(got.nan_to_num()), bits(want[t].nan_to_num()))
+    assert rows[0, :, 6].isnan().all() and (rows.float().nan_to_num() == 3).sum() == 2 * (48 - 5) * 128
+
+
+@pytest.mark.parametrize("size,eps", [(1e30, 1e-6), (1e-30, 0.0), (1e-42, 0.0), (3e38, 0.0), (1e-30, 1e-6), (1.0, 3e38)])
+def test_sizes_at_the_ends_of_the_range(size, eps):
+    """The mean is taken in 64 bits, where no square overflows or vanishes."""
+    r = Rows(4, 2, 1, 64, 0, seed=7)
+    x = torch.from_numpy((np.random.default_rng(0).uniform(-1, 1, (4, 2, 64)) * size).astype(np.float32)).cuda()
+    r.q = x
+    call(r, 16, eps=eps)
+    want, got = torch.from_numpy(r.expected("q", eps)).bfloat16(), r.q_out.cpu()
+    assert torch.equal(got.isnan(), want.isnan())  # (a NaN's own bits say nothing: 0 times infinity)
+    assert torch.equal(bits(got[~got.isnan()]), bits(want[~got.isnan()]))
+    if eps == 0 and size >= 1e-30:  # (the root of 1e-84 has no inverse in fp32)
+        assert 0.1 < float(r.q_out.float().abs().mean()) < 1.5
+
+
+def test_rows_that_are_zero_infinite_or_nan():
+    r = Rows(5, 1, 1, 64, 0, seed=8)
+    q = torch.ones((5, 1, 64), device="cuda")
+    q[0] = 0
+    q[1, 0, 3] = float("inf")
+    q[2, 0, 5] = float("nan")
+    q[3, 0, 9] = float("-inf")
+    r.q = q
+    call(r, 16, eps=0.0)
+    got = r.q_out.float().cpu()
+    assert got[0].isnan().all()                   # 0 over the root of 0
+    for t, at in ((1, 3), (3, 9)):                # the root is infinite: what is finite becomes 0
+        assert got[t, 0, at].isnan() and (got[t, 0, torch.arange(64) != at] == 0).all()
+    assert got[2].isnan().all() and got[4].isfinite().all()
+    call(r, 16, eps=1e-6)
+    assert (r.q_out.float().cpu()[0] == 0).all()
+
+
+def test_captured_and_replayed():
+    r = Rows(9, 8, 2, 128, 128, seed=9)
+    ref = [call(r, 16, eps=1e-5)[0].clone(), r.q_out.clone()]
+    nb, d = 3, B.attn_dims(0, 8, 2, 128, 16, 1, 3)
+    slots = i32(np.random.default_rng(3).permutation(nb * 16)[:9])
+    k, v = (torch.full((nb, 2, 16, 128), 3.0, device="cuda").bfloat16() for _ in "kv")
+
+    def go():
+        B.moe_kv_append_norm(r.q, r.k, r.v, r.positions, r.axis, r.cos, r.sin, slots, d, r.q_out, k, v, r.q_norm, r.k_norm, eps=1e-5)
+
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        go()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        go()
+    for _ in range(3):
+        k.fill_(3.0)
+        r.q_out.fill_(0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(bits(k), bits(ref[0])) and torch.equal(bits(r.q_out), bits(ref[1]))
