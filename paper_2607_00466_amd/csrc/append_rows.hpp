@@ -7,22 +7,30 @@
 
 namespace eldr {
 
+// Eight consecutive values on their way.
+template <typename In>
+struct Raw8 {
+  static constexpr int kWords = 2 * sizeof(In);
+  u32x4 raw[kWords / 4];
+  __device__ __forceinline__ void load(const In* p) {
+#pragma unroll
+    for (int i = 0; i < kWords / 4; ++i) raw[i] = reinterpret_cast<const u32x4*>(p)[i];
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (sizeof(In) == 4) x[i] = __uint_as_float(raw[i / 4][i % 4]);
+      else x[i] = __uint_as_float(i % 2 ? raw[0][i / 2] & 0xffff0000u : raw[0][i / 2] << 16);
+    }
+  }
+};
+
 // Eight consecutive values as fp32.
 template <typename In>
 __device__ __forceinline__ void load8(const In* p, float (&x)[8]) {
-  if constexpr (sizeof(In) == 4) {
-    const f32x4 a = *reinterpret_cast<const f32x4*>(p);
-    const f32x4 b = *reinterpret_cast<const f32x4*>(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-  } else {
-    const u32x4 a = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(a[i] << 16);
-      x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
-    }
-  }
+  Raw8<In> r;
+  r.load(p);
+  r.get(x);
 }
 
 __device__ __forceinline__ void store8_bf16(uint16_t* p, const float (&x)[8]) {

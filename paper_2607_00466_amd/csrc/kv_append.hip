@@ -32,7 +32,7 @@ struct AppendArgs {
 };
 
 template <typename In, bool FP8, bool INTERLEAVED, bool NORM>
-__global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(
+__global__ __launch_bounds__(kAppendThreads, NORM ? (FP8 ? 5 : 6) : 8) void kv_append_kernel(
     AppendArgs a, Pages pg, const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride,
     int64_t v_stride, const float* k_scale, const float* v_scale, void* k_cache, void* v_cache) {
   const int64_t id = (int64_t)blockIdx.x * kAppendThreads + threadIdx.x;

@@ -31,7 +31,7 @@ struct QuantArgs {
   float eps;
   int32_t R, Hq;
   int32_t unit_shift, unit_more;  // unit_of
-  int32_t tiles, tile_blocks;     // units * 2 * Hkv, and the workgroups they take
+  int32_t tiles, tile_blocks;     // units * 2 Hkv, and the workgroups they take
   int32_t q_lanes;                // threads that share a token's queries
   // Units before those of request r, whose tokens begin at `start`: a unit for each
   // token, or one for each whole page of tokens before and two more a request.  (n
@@ -44,10 +44,15 @@ struct QuantArgs {
 // does); by one wave.
 template <typename F>
 __device__ __forceinline__ int last_request(int R, int most, F f) {
+  constexpr int kBatch = 4;  // loads in flight
   int count = 0;
-  for (int r0 = 0; r0 < R; r0 += kWave) {
-    const int r = r0 + (int)(threadIdx.x % kWave);
-    count += __popcll(__ballot(r < R && f(min(r, R - 1)) <= most));
+  for (int r0 = 0; r0 < R; r0 += kBatch * kWave) {
+    int at[kBatch];
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) at[b] = f(min(r0 + b * kWave + (int)(threadIdx.x % kWave), R - 1));
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b)
+      count += __popcll(__ballot(r0 + b * kWave + (int)(threadIdx.x % kWave) < R && at[b] <= most));
   }
   return max(count - 1, 0);
 }
@@ -72,19 +77,32 @@ __device__ __forceinline__ float grown(float scale, float top, float& back) {
   return (float)ldexp((double)scale, n);
 }
 
-// round(x / scale) within +-127 as four codes' bytes; 0 where the scale is 0, or NaN
-__device__ __forceinline__ uint32_t code_of(float x, float scale) {
-  const float c = fminf(fmaxf(rintf(x / scale), -127.0f), 127.0f);
-  return (uint32_t)(scale > 0.0f ? (int)c : 0) & 0xffu;
-}
-__device__ __forceinline__ u32x2 codes8(const float (&x)[8], float scale) {
-  u32x2 v;
+// What turns values into codes of a page.
+struct Coder {
+  float by, scale, inverse;  // values times `by` are in units of `scale`
+  bool none;                 // the scale is 0, or NaN
+  // (2^64: where the scale's inverse would be infinite, or a remainder below fp32's range)
+  __device__ __forceinline__ explicit Coder(float page_scale)
+      : by(page_scale < 0x1p-60f ? 0x1p64f : 1.0f), scale(page_scale * by), inverse(1.0f / scale), none(!(page_scale > 0.0f)) {}
+  // round(x / scale) within +-127.  The quotient is the correctly rounded one, so that
+  // codes equal those of the definition: two steps from the product with the inverse.
+  // (No magnitude is over 127 scale and its rounding; quotients too small for the
+  // steps to be exact round to 0.)
+  __device__ __forceinline__ uint32_t code(float x) const {
+    x *= by;
+    float c = x * inverse;
+    c = fmaf(fmaf(-c, scale, x), inverse, c);
+    c = fmaf(fmaf(-c, scale, x), inverse, c);
+    c = fminf(fmaxf(rintf(c), -127.0f), 127.0f);
+    return (uint32_t)(none ? 0 : (int)c) & 0xffu;
+  }
+  __device__ __forceinline__ u32x2 codes(const float (&x)[8]) const {
+    u32x2 v;
 #pragma unroll
-  for (int w = 0; w < 2; ++w)
-    v[w] = code_of(x[4 * w], scale) | code_of(x[4 * w + 1], scale) << 8 | code_of(x[4 * w + 2], scale) << 16 |
-           code_of(x[4 * w + 3], scale) << 24;
-  return v;
-}
+    for (int w = 0; w < 2; ++w) v[w] = code(x[4 * w]) | code(x[4 * w + 1]) << 8 | code(x[4 * w + 2]) << 16 | code(x[4 * w + 3]) << 24;
+    return v;
+  }
+};
 
 // Held codes under a scale that is 2^n as large: back = 2^-n.
 __device__ __forceinline__ u32x4 codes_again(u32x4 old, float back) {
@@ -102,36 +120,24 @@ __device__ __forceinline__ u32x4 codes_again(u32x4 old, float back) {
   return v;
 }
 
-// A tile's new rows: `rows` of them from token t0 on, to offsets from o0 on.
+// A page's new rows: `rows` of them from token t0 on, to offsets from o0 on.
 struct PageRows {
-  int t0, o0, rows;
+  int page, t0, o0, rows;
 };
 
-// WAVES: of a tile.
+// One tile: the rows of kind `kind`, a kv head's keys (below Hkv) or values, by
+// WAVES waves.
 template <typename In, int D, bool INTERLEAVED, int WAVES>
-__device__ __forceinline__ void quantise_tile(const QuantArgs& a, const Pages& pg, uint32_t* tops) {
+__device__ __forceinline__ void quantise_tile(const QuantArgs& a, const Pages& pg, const PageRows& p, int kind, uint32_t* tops) {
   constexpr int kLanes = D / 16;                       // of a row
   constexpr int kRowsPass = WAVES * kWave / kLanes;    // 64 / kLanes a wave
   constexpr int kHold = kLanes / 4;                    // passes in registers: 16 rows a wave
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int tile = WAVES == 1 ? blockIdx.x * (kQuantThreads / kWave) + wave : blockIdx.x;
-  if (tile >= a.tiles) return;
-  const int kinds = 2 * pg.Hkv, u = tile / kinds, kind = tile - u * kinds;
+  const int id = threadIdx.x % (WAVES * kWave), chunk = id % kLanes, row0 = id / kLanes;
+  const int wave = threadIdx.x / kWave;
   const bool is_v = kind >= pg.Hkv;
   const int h = is_v ? kind - pg.Hkv : kind;
-  const int r = last_request(a.R, u, [&](int i) { return a.unit_of(i, a.start_of(i)); });
-  PageRows p;
-  const int start = a.start_of(r), tokens = max(a.start_of(r + 1) - start, 0);
-  const int held = min(max(a.lens[r], 0), pg.capacity());
-  const int page_at = (held >> pg.shift) + u - a.unit_of(r, start);  // of the request's pages
-  if (u < a.unit_of(r, start) || page_at >= pg.max_blocks) return;
-  const int first = max(held, page_at << pg.shift), end = min(held + tokens, (page_at + 1) << pg.shift);
-  if (first >= end) return;
-  const int page = pg.table[(int64_t)r * pg.max_blocks + page_at];
-  if (!pg.has(page)) return;
-  p.t0 = start + first - held, p.o0 = first & ((1 << pg.shift) - 1), p.rows = end - first;
-
-  const int id = threadIdx.x % (WAVES * kWave), chunk = id % kLanes, row0 = id / kLanes;
+  float* scale_at = (is_v ? a.v_scale : a.k_scale) + (int64_t)p.page * pg.Hkv + h;
+  const float old = p.o0 > 0 ? *scale_at : 0.0f;
   const bool turns = !is_v && chunk * 16 < a.turns.rot;
   const Runs at(chunk, a.turns.rot / 2, turns && !INTERLEAVED);
   const float* weight = is_v ? nullptr : a.k_norm;
@@ -144,18 +150,20 @@ __device__ __forceinline__ void quantise_tile(const QuantArgs& a, const Pages& p
   const int64_t stride = is_v ? a.v_stride : a.k_stride;
   const auto load = [&](int row, float (&x)[8], float (&y)[8]) {
     const int t = p.t0 + row;
-    load8(src + t * stride + at.e0, x);
-    load8(src + t * stride + at.e1, y);
+    // what the row needs is asked for before any of it is worked on
+    Raw8<In> r[2];
+    r[0].load(src + t * stride + at.e0);
+    r[1].load(src + t * stride + at.e1);
+    float c[8], s[8];
+    if (turns) load_angles(a.turns, t, chunk, c, s);
+    r[0].get(x);
+    r[1].get(y);
     if (weight) {
       const float i = row_scale(x, y, kLanes, a.eps);
       norm8(x, i, wx);
       norm8(y, i, wy);
     }
-    if (turns) {
-      float c[8], s[8];
-      load_angles(a.turns, t, chunk, c, s);
-      turn_runs<INTERLEAVED>(x, y, c, s);
-    }
+    if (turns) turn_runs<INTERLEAVED>(x, y, c, s);
   };
   uint32_t top = 0;  // largest magnitude's bits: a NaN's are above infinity's
   const auto see = [&](const float (&x)[8]) {
@@ -185,24 +193,23 @@ __device__ __forceinline__ void quantise_tile(const QuantArgs& a, const Pages& p
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) top = max(top, tops[w]);
   }
-  float* scale_at = (is_v ? a.v_scale : a.k_scale) + (int64_t)page * pg.Hkv + h;
-  const float old = p.o0 > 0 ? *scale_at : 0.0f;
   float scale = __uint_as_float(top) * (1.0f / 127.0f), back = 0.0f;
   if (old > 0.0f && top < 0x7f800000u) scale = grown(old, __uint_as_float(top), back);
   const bool finite = top < 0x7f800000u && (__float_as_uint(old) & 0x7fffffffu) < 0x7f800000u;
   if (!finite) scale = __builtin_nanf("");
   if constexpr (WAVES > 1) __syncthreads();  // (the old scale is read before the new one is written)
   if (id == 0) *scale_at = scale;
-  int8_t* rows_at = (is_v ? a.v_cache : a.k_cache) + pg.row(page, h, p.o0);
+  int8_t* rows_at = (is_v ? a.v_cache : a.k_cache) + pg.row(p.page, h, p.o0);
   // held rows, where the scale changed: from the page's first slot on
   if (p.o0 > 0 && finite && back != 1.0f) {
     u32x4* piece = reinterpret_cast<u32x4*>(rows_at - p.o0 * D);
     for (int i = id; i < p.o0 * kLanes; i += WAVES * kWave) piece[i] = codes_again(piece[i], back);
   }
+  const Coder coder(scale);
   const auto store = [&](int row, const float (&x)[8], const float (&y)[8]) {
     int8_t* dst = rows_at + row * D;
-    *reinterpret_cast<u32x2*>(dst + at.e0) = codes8(x, scale);
-    *reinterpret_cast<u32x2*>(dst + at.e1) = codes8(y, scale);
+    *reinterpret_cast<u32x2*>(dst + at.e0) = coder.codes(x);
+    *reinterpret_cast<u32x2*>(dst + at.e1) = coder.codes(y);
   };
 #pragma unroll
   for (int i = 0; i < kHold; ++i) {
@@ -214,6 +221,29 @@ __device__ __forceinline__ void quantise_tile(const QuantArgs& a, const Pages& p
     load(row, x, y);
     store(row, x, y);
   }
+}
+
+// A wave's (or workgroup's) tile: which page and rows it is.
+template <typename In, int D, bool INTERLEAVED, int WAVES>
+__device__ __forceinline__ void quantise_page(const QuantArgs& a, const Pages& pg, uint32_t* tops) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int tile = WAVES == 1 ? blockIdx.x * (kQuantThreads / kWave) + wave : blockIdx.x;
+  if (tile >= a.tiles) return;
+  const int kinds = 2 * pg.Hkv, u = tile / kinds;
+  // (a decode batch: request u's own token)
+  int r = min(u, a.R - 1);
+  if (a.unit_more != 0 || a.start_of(r) > u || a.start_of(r + 1) <= u)
+    r = last_request(a.R, u, [&](int i) { return a.unit_of(i, a.start_of(i)); });
+  const int start = a.start_of(r), tokens = max(a.start_of(r + 1) - start, 0);
+  const int held = min(max(a.lens[r], 0), pg.capacity());
+  const int page_at = (held >> pg.shift) + u - a.unit_of(r, start);  // of the request's pages
+  if (u < a.unit_of(r, start) || page_at >= pg.max_blocks) return;
+  const int first = max(held, page_at << pg.shift), end = min(held + tokens, (page_at + 1) << pg.shift);
+  if (first >= end) return;
+  const int page = pg.table[(int64_t)r * pg.max_blocks + page_at];
+  if (!pg.has(page)) return;
+  const PageRows p{page, start + first - held, first & ((1 << pg.shift) - 1), end - first};
+  quantise_tile<In, D, INTERLEAVED, WAVES>(a, pg, p, tile - u * kinds, tops);
 }
 
 // Queries: as in moe_kv_append, several heads a thread with the angles it has read.
@@ -251,7 +281,7 @@ __device__ __forceinline__ void turn_queries(const QuantArgs& a, int block) {
 template <typename In, int D, bool INTERLEAVED, int WAVES>
 __global__ __launch_bounds__(kQuantThreads) void kv_append_int8_kernel(QuantArgs a, Pages pg) {
   __shared__ uint32_t tops[kQuantThreads / kWave];
-  if ((int)blockIdx.x < a.tile_blocks) quantise_tile<In, D, INTERLEAVED, WAVES>(a, pg, tops);
+  if ((int)blockIdx.x < a.tile_blocks) quantise_page<In, D, INTERLEAVED, WAVES>(a, pg, tops);
   else turn_queries<In, D, INTERLEAVED>(a, blockIdx.x - a.tile_blocks);
 }
 

@@ -171,3 +171,28 @@ def test_on_two_streams_at_once():
         append_int8(r, c, [0, 300], table, [5], stream=s)
     for r, c, before, _ in calls:
         check_append_int8(r, c, before, [0, 300], table, [5])
+
+
+@pytest.mark.parametrize("top", [1.0, 3.7e-3, 811.3, 2.0 ** -100, 1.1e-41, 3.3e38])
+def test_values_at_the_borders_between_codes(top):
+    """Half steps and the fp32 numbers around them: the quotient that is rounded is the
+    correctly rounded one."""
+    top = np.float32(top)
+    scale = top * (np.float32(1) / np.float32(127))
+    x = ((np.arange(0, 127) + np.float32(0.5)) * scale).astype(np.float32)
+    near = [x]
+    for _ in range(4):
+        near += [np.nextafter(near[-1], np.float32(np.inf))]
+    down = x
+    for _ in range(4):
+        down = np.nextafter(down, np.float32(-np.inf))
+        near += [down]
+    x = np.concatenate(near).astype(np.float32)
+    x = np.minimum(np.concatenate([x, -x, np.full(-2 * len(x) % 64, top, np.float32)]), top)
+    x[::64] = top  # every row has the largest value
+    r = Rows(len(x) // 64, 1, 1, 64, 0, norms=False, seed=9)
+    r.v = torch.from_numpy(x.reshape(-1, 1, 64)).cuda()
+    c = Int8Cache(3, 1, 16, 64, seed=10)
+    before = c.numpy()
+    append_int8(r, c, [0, r.T], [[2, 0, 1]], [0])
+    check_append_int8(r, c, before, [0, r.T], [[2, 0, 1]], [0])
