@@ -752,10 +752,12 @@ def _need_scales(k_scale, v_scale, d: AttnDims) -> None:
     _need_opt(v_scale, "v_scale", torch.float32, d.Hkv)
 
 
-def _need_here(t: torch.Tensor, name: str) -> None:
-    """Kernels run on the current device."""
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name}: is on {t.device}, and the current device is cuda:{torch.cuda.current_device()}")
+def _stream_here(stream, t: torch.Tensor, name: str) -> int:
+    """_stream, of the current device, which t has to be on: kernels run there."""
+    here = torch.cuda.current_device()
+    if t.device.index != here:
+        raise ValueError(f"{name}: is on {t.device}, and the current device is cuda:{here}")
+    return _raw_stream(here) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 def _need_rows(t: torch.Tensor, name: str, T: int, heads: int, D: int) -> int:
@@ -790,13 +792,15 @@ def _need_groups(group_start, prefix_len) -> int:
 def _append_rows(q, k, v, T: int, positions, pair_axis, cos, sin, d: AttnDims, q_out, interleaved: bool):
     """What the appends' calls begin with: rows, their strides and type, T, rotation."""
     Hq, Hkv, D = d.Hq, d.Hkv, d.D
-    if positions.dim() != 2 or positions.shape[1] != T:
+    n_axes, cols = positions.shape if positions.dim() == 2 else (0, -1)
+    if cols != T:
         raise ValueError(f"positions: expected [n_axes, {T}]")
-    if cos.dim() != 2 or cos.shape != sin.shape:
+    shape = cos.shape
+    if len(shape) != 2 or shape != sin.shape:
         raise ValueError("cos, sin: expected two [max_pos, rot / 2] tensors")
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out come together")
-    n_axes, (max_pos, half) = positions.shape[0], cos.shape
+    max_pos, half = shape
     if pair_axis.numel() != half:
         raise ValueError(f"pair_axis: expected {half} axes, one a pair")
     dtype = k.dtype
@@ -809,10 +813,14 @@ def _append_rows(q, k, v, T: int, positions, pair_axis, cos, sin, d: AttnDims, q
         pq, pq_out = q.data_ptr(), q_out.data_ptr()
     k_stride, v_stride = _need_rows(k, "k", T, Hkv, D), _need_rows(v, "v", T, Hkv, D)
     i32, f32 = torch.int32, torch.float32
-    _need(positions, "positions", i32, n_axes * T)
-    _need(pair_axis, "pair_axis", i32, half)
-    _need(cos, "cos", f32, max_pos * half)
-    _need(sin, "sin", f32, max_pos * half)
+    # (their sizes are known by now: one expression where they pass)
+    if not (positions.is_cuda and positions.dtype is i32 and positions.is_contiguous() and pair_axis.is_cuda and
+            pair_axis.dtype is i32 and pair_axis.is_contiguous() and cos.is_cuda and cos.dtype is f32 and
+            cos.is_contiguous() and sin.is_cuda and sin.dtype is f32 and sin.is_contiguous()):
+        _need(positions, "positions", i32, n_axes * T)
+        _need(pair_axis, "pair_axis", i32, half)
+        _need(cos, "cos", f32, max_pos * half)
+        _need(sin, "sin", f32, max_pos * half)
     return (pq, k.data_ptr(), v.data_ptr(), q_stride, k_stride, v_stride, _IN_TYPES[dtype], T, positions.data_ptr(), n_axes,
             pair_axis.data_ptr(), cos.data_ptr(), sin.data_ptr(), max_pos, 2 * half, 1 if interleaved else 0), pq_out
 
@@ -849,10 +857,11 @@ def moe_kv_append_norm(q, k, v, positions, pair_axis, cos, sin, slots, d: AttnDi
     _need_opt(v_scale, "v_scale", torch.float32, d.Hkv)
     _need_cache(k_cache, "k_cache", d)
     _need_cache(v_cache, "v_cache", d)
-    _need_here(k_cache, "k_cache")
-    _check("moe_kv_append_norm", load().moe_kv_append_norm(
+    status = load().moe_kv_append_norm(
         *rows, slots.data_ptr(), d, _ptr(q_norm), _ptr(k_norm), eps, _ptr(k_scale), _ptr(v_scale), pq_out, k_cache.data_ptr(),
-        v_cache.data_ptr(), _stream(stream)))
+        v_cache.data_ptr(), _stream_here(stream, k_cache, "k_cache"))
+    if status:
+        _check("moe_kv_append_norm", status)
 
 
 def moe_kv_append_int8(q, k, v, positions, pair_axis, cos, sin, query_start, block_table, lens, d: AttnDims, q_out, k_cache,
@@ -872,35 +881,35 @@ def moe_kv_append_int8(q, k, v, positions, pair_axis, cos, sin, query_start, blo
     _need_cache(k_cache, "k_cache", d)
     _need_cache(v_cache, "v_cache", d)
     _need_scales(k_scale, v_scale, d)
-    _need_here(k_cache, "k_cache")
-    _check("moe_kv_append_int8", load().moe_kv_append_int8(
+    status = load().moe_kv_append_int8(
         *rows, query_start.data_ptr(), block_table.data_ptr(), lens.data_ptr(), d, _ptr(q_norm), _ptr(k_norm), eps, pq_out,
-        k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), _stream(stream)))
+        k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _stream_here(stream, k_cache, "k_cache"))
+    if status:
+        _check("moe_kv_append_int8", status)
 
 
 def _need_layers(k_cache, v_cache, k_scale, v_scale, d: AttnDims):
     """The caches of one layer, or [layers, ...] of several: their count and stride."""
-    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        if not isinstance(t, torch.Tensor):
-            raise TypeError(f"{name}: expected a torch tensor")
-        if t.dim() == 4:
-            _need_cache(t, name, d)
-        elif t.dim() != 5:
-            raise ValueError(f"{name}: expected [num_blocks, Hkv, block_size, D] or [layers, ...] of it, got {tuple(t.shape)}")
-    if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride():
-        raise ValueError("k_cache and v_cache: expected the same shape and strides")
     layers, stride = 1, 0
-    if k_cache.dim() == 5:
-        layers, stride = k_cache.shape[0], k_cache.stride(0)
-        if layers > 0:
-            for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+    if isinstance(k_cache, torch.Tensor) and k_cache.dim() == 4:
+        _need_cache(k_cache, "k_cache", d)
+        _need_cache(v_cache, "v_cache", d)
+    else:
+        for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{name}: expected a torch tensor")
+            if t.dim() != 5:
+                raise ValueError(f"{name}: expected [num_blocks, Hkv, block_size, D] or [layers, ...] of it, got {tuple(t.shape)}")
+            if t.shape[0] > 0:
                 _need_cache_rows(t[0], name, d)
-        if layers == 1 or k_cache.numel() == 0:
-            stride = 0  # of no use
+        layers, strides = k_cache.shape[0], k_cache.stride()
+        if v_cache.shape[0] != layers or v_cache.stride() != strides:
+            raise ValueError("k_cache and v_cache: expected the same shape and strides")
+        if layers > 1 and d.num_blocks > 0:  # (else it is of no use)
+            stride = strides[0]
     if d.kv_type == MOE_KV_INT8:
-        for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
-            _need(t, name, torch.float32, layers * d.num_blocks * d.Hkv)
-    _need_here(k_cache, "k_cache")
+        _need(k_scale, "k_scale", torch.float32, layers * d.num_blocks * d.Hkv)
+        _need(v_scale, "v_scale", torch.float32, layers * d.num_blocks * d.Hkv)
     return layers, stride
 
 
@@ -926,9 +935,11 @@ def moe_kv_fork(parent, child, page, block_table, lens, d: AttnDims, k_cache, v_
     _need(block_table, "block_table", i32, d.R * d.max_blocks)
     _need(lens, "lens", i32, d.R)
     layers, stride = _need_layers(k_cache, v_cache, k_scale, v_scale, d)
-    _check("moe_kv_fork", load().moe_kv_fork(
+    status = load().moe_kv_fork(
         parent.data_ptr(), child.data_ptr(), page.data_ptr(), F, block_table.data_ptr(), lens.data_ptr(), d, layers, stride,
-        k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), _stream(stream)))
+        k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), _stream_here(stream, k_cache, "k_cache"))
+    if status:
+        _check("moe_kv_fork", status)
 
 
 def moe_kv_compact(remap, block_table, table_out, d: AttnDims, k_cache, v_cache, k_scale=None, v_scale=None,
@@ -941,9 +952,11 @@ def moe_kv_compact(remap, block_table, table_out, d: AttnDims, k_cache, v_cache,
     _need(block_table, "block_table", i32, d.R * d.max_blocks)
     _need(table_out, "table_out", i32, d.R * d.max_blocks)
     layers, stride = _need_layers(k_cache, v_cache, k_scale, v_scale, d)
-    _check("moe_kv_compact", load().moe_kv_compact(
+    status = load().moe_kv_compact(
         remap.data_ptr(), block_table.data_ptr(), table_out.data_ptr(), d, layers, stride, k_cache.data_ptr(),
-        v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), _stream(stream)))
+        v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), _stream_here(stream, k_cache, "k_cache"))
+    if status:
+        _check("moe_kv_compact", status)
 
 
 def moe_attn_workspace_bytes(d: AttnDims) -> int:
