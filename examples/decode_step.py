@@ -1,16 +1,22 @@
 """A decode worker's steps on one layer: attention over the paged KV cache, then the
 MoE layer, for a batch whose requests share their domain's prompt.
 
-    python examples/decode_step.py [--requests 64] [--prefix 2048] [--own 256] [--budget 2304] [--steps 20] [--fp8]
+    python examples/decode_step.py [--requests 64] [--prefix 2048] [--own 256] [--budget 2304] [--steps 20]
+                                   [--fp8 | --int8] [--norm]
 
 Each step, all on one stream and without a host synchronisation:
 
   1. project the batch's hidden states to queries, keys and values
   2. moe_kv_append    rotate them by their positions, store keys and values
+                      (--norm: moe_kv_append_norm, queries and keys normed first;
+                      --int8: moe_kv_append_int8, into 8-bit integers)
   3. moe_attn_decode  attend; the shared prompt is read once for its group
   4. project back, and run the MoE layer (moe_layer)
   5. moe_attn_weights add to each cached token's accumulated attention weight
   6. moe_kv_evict     requests over their budget lose their lightest tokens
+
+A cache of 8-bit integers has a scale for each page and does without 5 and 6, so the
+budget has to hold every step's token.
 
 Random weights and hidden states; the projections are torch's, everything else is
 the library's.
@@ -45,11 +51,13 @@ class Worker:
     for `steps` steps."""
 
     def __init__(self, shape: synth.LayerShape, heads: Heads, R: int, groups: int, prefix: int, own: int, budget: int,
-                 steps: int, recent: int = 32, fp8: bool = False, seed: int = 0):
+                 steps: int, recent: int = 32, fp8: bool = False, int8: bool = False, norm: bool = False, seed: int = 0):
         if prefix % BLOCK or budget < prefix + recent:
             raise ValueError("the prefix is whole pages, and the budget holds it and the recent tokens")
         if steps < 1 or own < 0 or groups < 1:
             raise ValueError("a worker has a step to make, a group and no fewer than 0 tokens of its own a request")
+        if int8 and (fp8 or budget < prefix + own + steps):
+            raise ValueError("a cache of 8-bit integers is none of fp8, and nothing is evicted from it: the budget holds every token")
         self.left = steps
         self.shape, self.heads, self.budget, self.recent = shape, heads, budget, recent
         gen = torch.Generator(device="cuda").manual_seed(seed)
@@ -65,6 +73,7 @@ class Worker:
             1e6 ** (-torch.arange(D // 2, device="cuda", dtype=torch.float64) * 2 / D)
         self.cos, self.sin = angle.cos().float(), angle.sin().float()
         self.pair_axis = torch.zeros(D // 2, **i32)  # text: one position axis
+        self.q_norm, self.k_norm = (1 + normal(D, std=0.1) if norm else None for _ in "qk")
         # pages: each group's shared ones, then each request's own (room for every step, or for the budget and one more)
         most = min(prefix + own + steps, max(budget, prefix + own) + 1)
         shared, private = prefix // BLOCK, -(-(most - prefix) // BLOCK)
@@ -79,10 +88,13 @@ class Worker:
         self.group_start = torch.tensor(start, **i32)
         self.prefix_len = torch.full((groups,), prefix, **i32)
         self.protect = torch.full((R,), prefix, **i32)
-        kv = torch.float8_e4m3fn if fp8 else torch.bfloat16
+        kv = torch.int8 if int8 else torch.float8_e4m3fn if fp8 else torch.bfloat16
         self.d = B.attn_dims(R, Hq, Hkv, D, BLOCK, table.shape[1], nb, kv)
         self.k_cache, self.v_cache = (torch.zeros((nb, Hkv, BLOCK, D), device="cuda").to(kv) for _ in "kv")
         self.k_scale = self.v_scale = torch.full((Hkv,), 1 / 64, device="cuda") if fp8 else None
+        if int8:
+            self.k_scale, self.v_scale = (torch.zeros((nb, Hkv), device="cuda") for _ in "kv")
+        self.int8 = int8
         self.N = table.shape[1] * BLOCK
         # per slot: the token's position, and the attention it has received
         self.pos = torch.full((R, Hkv, self.N), -1, **i32)
@@ -97,15 +109,31 @@ class Worker:
         self.moe_d = B.dims(R, H, shape.E, shape.K, shape.I)
         self.moe = B.LayerBuffers.allocate(self.moe_d)
         self.rows = torch.arange(R, device="cuda")
+        self.each = torch.arange(R + 1, **i32)  # a token of each request
         self._prompt(normal, start, prefix, own)
 
-    def _append(self, x, positions, slots, q_out):
-        """Project x [T, H] and store its keys and values; queries into q_out where wanted."""
-        h = self.heads
-        qkv = (x.bfloat16() @ self.w_qkv).view(x.shape[0], h.Hq + 2 * h.Hkv, h.D)
+    def _append(self, x, positions, rows, index, q_out):
+        """Project x [T, H] and store its keys and values at slots `index` of requests
+        `rows` (one, or one a token); queries into q_out where wanted."""
+        h, T = self.heads, x.shape[0]
+        if T == 0:
+            return
+        qkv = (x.bfloat16() @ self.w_qkv).view(T, h.Hq + 2 * h.Hkv, h.D)
         q = qkv[:, :h.Hq] if q_out is not None else None
-        B.moe_kv_append(q, qkv[:, h.Hq:h.Hq + h.Hkv], qkv[:, h.Hq + h.Hkv:], positions[None], self.pair_axis, self.cos,
-                        self.sin, slots, self.d, q_out, self.k_cache, self.v_cache, self.k_scale, self.v_scale)
+        new = (q, qkv[:, h.Hq:h.Hq + h.Hkv], qkv[:, h.Hq + h.Hkv:], positions[None], self.pair_axis, self.cos, self.sin)
+        if self.int8:
+            one = isinstance(rows, int)  # a run of tokens of one request, or a token of each
+            table = self.table[rows:rows + 1] if one else self.table
+            d = B.attn_dims(len(table), h.Hq, h.Hkv, h.D, BLOCK, self.d.max_blocks, self.d.num_blocks, torch.int8)
+            start = torch.tensor([0, T], dtype=torch.int32, device="cuda") if one else self.each
+            B.moe_kv_append_int8(*new, start, table, index[:1].int() if one else index.int(), d, q_out, self.k_cache, self.v_cache,
+                                 self.k_scale, self.v_scale, self.q_norm, self.k_norm)
+            return
+        after = (self._slots(rows, index), self.d, q_out, self.k_cache, self.v_cache)
+        if self.q_norm is not None:
+            B.moe_kv_append_norm(*new, *after, self.q_norm, self.k_norm, k_scale=self.k_scale, v_scale=self.v_scale)
+        else:
+            B.moe_kv_append(*new, *after, self.k_scale, self.v_scale)
 
     def _slots(self, rows, index):
         """Cache slots of slot `index` of requests `rows`."""
@@ -117,10 +145,10 @@ class Worker:
         for g in range(len(start) - 1):
             at = torch.arange(prefix, device="cuda")
             if prefix:
-                self._append(normal(prefix, H), at.int(), self._slots(start[g], at), None)
+                self._append(normal(prefix, H), at.int(), start[g], at, None)
         for r in range(self.d.R):
             at = torch.arange(prefix, prefix + own, device="cuda")
-            self._append(normal(own, H), at.int(), self._slots(r, at), None)
+            self._append(normal(own, H), at.int(), r, at, None)
         self.pos[:, :, :prefix + own] = torch.arange(prefix + own, device="cuda", dtype=torch.int32)
         self.lens.fill_(prefix + own)
         self.seen.fill_(prefix + own)
@@ -131,7 +159,7 @@ class Worker:
             raise RuntimeError("the cache and the rotation tables have room for no further step")
         self.left -= 1
         at = self.lens.long()
-        self._append(x, self.seen, self._slots(self.rows, at), self.q)
+        self._append(x, self.seen, self.rows, at, self.q)
         self.pos[self.rows, :, at] = self.seen[:, None]
         self.lens += 1
         self.seen += 1
@@ -141,6 +169,8 @@ class Worker:
 
     def evict(self):
         """Steps 5 and 6."""
+        if self.int8:
+            return
         B.moe_attn_weights(self.q, self.k_cache, self.table, self.lens, self.lse, self.d, self.weights, self.weights,
                            self.group_start, self.prefix_len, self.k_scale)
         B.moe_kv_evict(self.weights, self.pos, self.lens, self.seen, self.table, self.d, self.budget, self.recent,
@@ -166,8 +196,11 @@ def main(argv=None):
     p.add_argument("--budget", type=int, default=2304)
     p.add_argument("--steps", type=int, default=20)
     p.add_argument("--fp8", action="store_true")
+    p.add_argument("--int8", action="store_true")
+    p.add_argument("--norm", action="store_true")
     a = p.parse_args(argv)
-    w = Worker(synth.SHAPES[a.shape], Heads(*a.heads), a.requests, a.groups, a.prefix, a.own, a.budget, a.steps, fp8=a.fp8)
+    w = Worker(synth.SHAPES[a.shape], Heads(*a.heads), a.requests, a.groups, a.prefix, a.own, a.budget, a.steps, fp8=a.fp8,
+               int8=a.int8, norm=a.norm)
     x = torch.randn((a.requests, w.shape.H), device="cuda")
     y = w.step(x)
     torch.cuda.synchronize()

@@ -199,3 +199,13 @@ def test_binding_names_the_tensor(lib):
         B._need_layers(t, t, None, None, d())
     with pytest.raises(ValueError, match="k_scale and v_scale: a cache of torch.int8 has both"):
         B._need_scales(None, t, d())
+
+
+def test_the_example_evicts_nothing_of_8_bit_integers():
+    from examples import decode_step as E
+    from paper_2607_00466_amd import synth
+
+    for bad in (dict(budget=50), dict(fp8=True)):
+        sizes = dict(R=4, groups=2, prefix=32, own=16, budget=64, steps=3, recent=4, int8=True) | bad
+        with pytest.raises(ValueError, match="8-bit integers"):
+            E.Worker(synth.SHAPES["tiny"], E.Heads(4, 2, 64), **sizes)
