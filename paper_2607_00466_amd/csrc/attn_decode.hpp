@@ -302,15 +302,79 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void attn_decode_
   }
 }
 
-// Adds up the parts of a row that has several, and writes a row that has none.
-// THREADS threads (64, or 256 where there are few rows, each of them in many
-// parts) take a (request, query head): sets of D / 4 of them take a part, four
-// values each, and take the parts in turn, with a running maximum; the sets meet
-// in LDS.
+// The parts of a row (a request's query head): `shared` ones of its group's prefix,
+// then its own; the first of each by row, the others by the workgroups after w0.
+struct RowParts {
+  const float *shared, *shared_rest, *own, *own_rest;  // (own_rest, shared_rest: of the row's place in a tile)
+  int shared_parts, own_parts, shared_w0, own_w0;
+  int hq, h;  // the row's query head and kv head
+};
+
+template <int D>
+__device__ __forceinline__ RowParts parts_of(const DecodeArgs& a, const Pages& pg, const Parts& parts, int q_row) {
+  constexpr int kPitch = D + 4, kTileRows = SharedTile<D>::kRowsWg;
+  const int R = a.gr.R, n = a.gr.n;
+  const int* own = parts.plan;
+  const int *reach = own + R + 1, *group = reach + R, *shared = group + R;
+  const int r = q_row / a.Hq, hq = q_row - r * a.Hq, h = hq / a.G, i = hq - h * a.G;
+  const int own_row = own[R], tiles = own[r + 1] - own[r], mine = reach[r];
+  RowParts p{parts.shared + (int64_t)q_row * kPitch, parts.shared_rest, parts.own + (int64_t)q_row * kPitch,
+             parts.own_rest + (int64_t)(i % kRows) * kPitch, 0, 0, 0, 0, hq, h};
+  if (mine > 0) {
+    const int g = group[r];
+    const int row = (r - max(a.gr.start[g], 0)) * a.G + i, per = tiles_of(0, mine);
+    const int u0 = h * shared[n] + shared[g] + row / kTileRows * per;
+    const Deal deal(shared[n] * pg.Hkv, kSharedWgs);
+    p.shared_w0 = deal.owner(u0);
+    p.shared_parts = deal.owner(u0 + per - 1) - p.shared_w0 + 1;
+    p.shared_rest += (int64_t)(row % kTileRows) * kPitch;
+  }
+  if (tiles > 0) {
+    const Deal deal(own_row * pg.Hkv * a.head_tiles, decode_wgs(D));
+    const int u0 = (h * a.head_tiles + i / kRows) * own_row + own[r];
+    p.own_w0 = deal.owner(u0);
+    p.own_parts = deal.owner(u0 + tiles - 1) - p.own_w0 + 1;
+  }
+  return p;
+}
+
+template <int D>
+__device__ __forceinline__ const float* part_at(const RowParts& r, int p) {
+  constexpr int kPitch = D + 4;
+  if (p < r.shared_parts) return p == 0 ? r.shared : r.shared_rest + (int64_t)(r.shared_w0 + p) * SharedTile<D>::kRowsWg * kPitch;
+  p -= r.shared_parts;
+  return p == 0 ? r.own : r.own_rest + (int64_t)(r.own_w0 + p) * kRows * kPitch;
+}
+
+// A row's sums so far, of four of its values: maximum, sum of weights, values.  (fmaf,
+// so that every kernel that adds parts up rounds alike.)
+struct RowSums {
+  float top = -INFINITY, total = 0.0f;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ void add(float m, float l, const f32x4& v) {
+    const float m2 = fmaxf(top, m), base = m2 == -INFINITY ? 0.0f : m2;
+    const float f = exp2_fast(top - base), e = exp2_fast(m - base);
+    total = fmaf(total, f, l * e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] = fmaf(sum[i], f, v[i] * e);
+    top = m2;
+  }
+};
+
+template <int D, int KV>
+__device__ __forceinline__ void write_row(const DecodeArgs& a, int q_row, int hq, int h, int at, const RowSums& x) {
+  const RowEnd end = end_row(x.top, x.total, a.sinks ? a.sinks + hq : nullptr, KV == kKvFp8 && a.v_scale ? a.v_scale[h] : 1.0f);
+  const f32x4 o = x.sum * end.by;
+  *reinterpret_cast<u32x2*>(a.out + (int64_t)q_row * D + 4 * at) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+  if (at == 0 && a.lse) a.lse[q_row] = end.lse;
+}
+
+// Adds up the parts of a row that has several, and writes a row that has none.  For
+// few rows, each of them in many parts: THREADS threads (256, or 64) take a row, sets
+// of D / 4 of them its parts in turn, four values each, and the sets meet in LDS.
 template <int D, int KV, int THREADS>
 __global__ __launch_bounds__(kDecodeThreads) void attn_join_kernel(DecodeArgs a, Pages pg, Parts parts, int rows) {
   constexpr int kSet = D / 4, kSets = THREADS / kSet, kRowsWg = kDecodeThreads / THREADS;
-  constexpr int kPitch = D + 4;
   __shared__ f32x4 sums_of[kRowsWg][kSets][kSet];
   __shared__ float tops_of[kRowsWg][kSets], totals_of[kRowsWg][kSets];
   const int mine_row = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
@@ -318,78 +382,64 @@ __global__ __launch_bounds__(kDecodeThreads) void attn_join_kernel(DecodeArgs a,
   const int q_row = real ? blockIdx.x * kRowsWg + mine_row : 0;
   auto& sums = sums_of[mine_row];
   auto &tops = tops_of[mine_row], &totals = totals_of[mine_row];
-  const int R = a.gr.R, n = a.gr.n;
-  const int* own = parts.plan;
-  const int *reach = own + R + 1, *group = reach + R, *shared = group + R;
-  const int r = q_row / a.Hq, hq = q_row - r * a.Hq, h = hq / a.G, i = hq - h * a.G;
-  const int own_row = own[R], tiles = own[r + 1] - own[r], mine = reach[r];
-  // the row's parts: the first by row, the others by the workgroups after w0
-  int shared_parts = 0, shared_w0 = 0, shared_at = 0, own_parts = 0, own_w0 = 0;
-  constexpr int kTileRows = SharedTile<D>::kRowsWg;
-  if (mine > 0) {
-    const int g = group[r];
-    const int row = (r - max(a.gr.start[g], 0)) * a.G + i, per = tiles_of(0, mine);
-    const int u0 = h * shared[n] + shared[g] + row / kTileRows * per;
-    const Deal deal(shared[n] * pg.Hkv, kSharedWgs);
-    shared_w0 = deal.owner(u0);
-    shared_parts = deal.owner(u0 + per - 1) - shared_w0 + 1;
-    shared_at = row % kTileRows;
-  }
-  if (tiles > 0) {
-    const Deal deal(own_row * pg.Hkv * a.head_tiles, decode_wgs(D));
-    const int u0 = (h * a.head_tiles + i / kRows) * own_row + own[r];
-    own_w0 = deal.owner(u0);
-    own_parts = deal.owner(u0 + tiles - 1) - own_w0 + 1;
-  }
-  const bool written = !real || (own_parts == 1 && shared_parts == 0);  // by attn_decode
+  const RowParts r = parts_of<D>(a, pg, parts, q_row);
+  const bool written = !real || (r.own_parts == 1 && r.shared_parts == 0);  // by attn_decode
   const int set = threadIdx.x % THREADS / kSet, at = threadIdx.x % kSet;
-  const int64_t first = (int64_t)q_row * kPitch;
-  const auto part = [&](int p) -> const float* {
-    if (p < shared_parts)
-      return p == 0 ? parts.shared + first : parts.shared_rest + ((int64_t)(shared_w0 + p) * kTileRows + shared_at) * kPitch;
-    p -= shared_parts;
-    return p == 0 ? parts.own + first : parts.own_rest + ((int64_t)(own_w0 + p) * kRows + i % kRows) * kPitch;
-  };
-  const int count = written ? 0 : shared_parts + own_parts;
+  const int count = written ? 0 : r.shared_parts + r.own_parts;
   constexpr int kBatch = 4;  // parts that a set has in flight
-  float top = -INFINITY, total = 0.0f;
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  RowSums x;
   for (int p0 = set; p0 < count; p0 += kBatch * kSets) {
     f32x4 v[kBatch], ml[kBatch];
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
-      const float* from = part(min(p0 + b * kSets, count - 1));
+      const float* from = part_at<D>(r, min(p0 + b * kSets, count - 1));
       v[b] = *reinterpret_cast<const f32x4*>(from + 4 * at);
       ml[b] = *reinterpret_cast<const f32x4*>(from + D);
     }
 #pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      const bool there = p0 + b * kSets < count;
-      const float pm = there ? ml[b][0] : -INFINITY;
-      const float m2 = fmaxf(top, pm), base = m2 == -INFINITY ? 0.0f : m2;
-      const float f = exp2_fast(top - base), e = exp2_fast(pm - base);
-      total = total * f + ml[b][1] * e;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sum[i] = sum[i] * f + (there ? v[b][i] : 0.0f) * e;  // (0 times what is not there may be NaN)
-      top = m2;
-    }
+    for (int b = 0; b < kBatch; ++b)
+      if (p0 + b * kSets < count) x.add(ml[b][0], ml[b][1], v[b]);
   }
-  sums[set][at] = sum;
-  if (at == 0) tops[set] = top, totals[set] = total;
+  sums[set][at] = x.sum;
+  if (at == 0) tops[set] = x.top, totals[set] = x.total;
   __syncthreads();
   if (written || set != 0) return;
 #pragma unroll
-  for (int s = 1; s < kSets; ++s) {
-    const float m2 = fmaxf(top, tops[s]), base = m2 == -INFINITY ? 0.0f : m2;
-    const float f = exp2_fast(top - base), e = exp2_fast(tops[s] - base);
-    total = total * f + totals[s] * e;
-    sum = sum * f + sums[s][at] * e;
-    top = m2;
+  for (int s = 1; s < kSets; ++s) x.add(tops[s], totals[s], sums[s][at]);
+  write_row<D, KV>(a, q_row, r.hq, r.h, at, x);
+}
+
+// The same for many rows, of a few parts each: D / 4 threads take a row.  What finds
+// a row's parts (eight divisions) is then a wave's work for up to four rows, where a
+// wave a row spent most of its time (16,384 rows of 64: 15.5 -> 8 us).  The parts are
+// added as kWave / kSet sets would.
+template <int D, int KV>
+__global__ __launch_bounds__(kDecodeThreads) void attn_join_rows_kernel(DecodeArgs a, Pages pg, Parts parts, int rows) {
+  constexpr int kSet = D / 4, kSets = kWave / kSet;
+  const int q_row = blockIdx.x * (kDecodeThreads / kSet) + threadIdx.x / kSet, at = threadIdx.x % kSet;
+  if (q_row >= rows) return;
+  const RowParts r = parts_of<D>(a, pg, parts, q_row);
+  if (r.own_parts == 1 && r.shared_parts == 0) return;  // written by attn_decode
+  const int count = r.shared_parts + r.own_parts;
+  constexpr int kBatch = 8;  // parts in flight
+  RowSums x[kSets];
+  for (int p0 = 0; p0 < count; p0 += kBatch) {
+    f32x4 v[kBatch];
+    f32x2 ml[kBatch];
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      if (p0 + b >= count) break;
+      const float* from = part_at<D>(r, p0 + b);
+      v[b] = *reinterpret_cast<const f32x4*>(from + 4 * at);
+      ml[b] = *reinterpret_cast<const f32x2*>(from + D);
+    }
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b)
+      if (p0 + b < count) x[b % kSets].add(ml[b][0], ml[b][1], v[b]);
   }
-  const RowEnd end = end_row(top, total, a.sinks ? a.sinks + hq : nullptr, KV == kKvFp8 && a.v_scale ? a.v_scale[h] : 1.0f);
-  sum *= end.by;
-  *reinterpret_cast<u32x2*>(a.out + (int64_t)q_row * D + 4 * at) = u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
-  if (at == 0 && a.lse) a.lse[q_row] = end.lse;
+#pragma unroll
+  for (int s = 1; s < kSets; ++s) x[0].add(x[s].top, x[s].total, x[s].sum);
+  write_row<D, KV>(a, q_row, r.hq, r.h, at, x[0]);
 }
 
 // Raises a kernel's dynamic LDS limit where a launch needs more than the default.
@@ -414,16 +464,24 @@ int launch_decode(const DecodeArgs& a, const Pages& pg, float* ws, hipStream_t s
     hipLaunchKernelGGL((attn_shared_kernel<D, KV>), dim3(kSharedWgs), dim3(kSharedThreads), S::kBytes + scale_bytes(KV) + plan, s, sh, pg);
   }
   hipLaunchKernelGGL((attn_decode_kernel<D, KV>), dim3(decode_wgs(D)), dim3(kDecodeThreads), lds, s, a, pg, parts);
-  // measured (us, whole calls; 256 threads a row, 64): 64 rows of 131,000 slots 51, 59;
+  // Measured (us, whole calls; 256 threads a row, 64): 64 rows of 131,000 slots 51, 59;
   // 512 of 16,384 73, 74, and behind 8192 37, 43; 1024 of up to 8000 70, 69, and behind
   // 8192 40, 42; 2048 of up to 8000 138, 136; 8192 behind 2048 73, 54; 16,384 of up to
-  // 1500 92, 71
-  constexpr int64_t kFewRows = 1024;
-  if (rows <= kFewRows)
-    hipLaunchKernelGGL((attn_join_kernel<D, KV, 256>), dim3((unsigned)rows), dim3(kDecodeThreads), 0, s, a, pg, parts, (int)rows);
-  else
-    hipLaunchKernelGGL((attn_join_kernel<D, KV, 64>), dim3((unsigned)((rows + 3) / 4)), dim3(kDecodeThreads), 0, s, a, pg, parts,
-                       (int)rows);
+  // 1500 92, 71.  D / 4 threads a row against 64: D = 64, 16,384 rows behind 8 x 2048 88.8,
+  // 95.7, of up to 1500 52.3, 57.0, 4096 of up to 700 16.1, 17.0, behind 8192 52.8, 52.8;
+  // D = 128, 8192 of up to 1500 49.7, 51.8, 4096 of up to 8000 103.4, 103.9, behind 4 x 2048
+  // 51.8, 49.8, 2048 behind 8192 51.5, 49.9; D = 256 the same.
+  constexpr int64_t kFewRows = 1024, kManyRows = D == 64 ? kFewRows : 4096;
+  const auto join = [&](auto kernel, int rows_wg) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + rows_wg - 1) / rows_wg)), dim3(kDecodeThreads), 0, s, a, pg, parts, (int)rows);
+  };
+  if (rows <= kFewRows) {
+    join(attn_join_kernel<D, KV, 256>, 1);
+  } else if (rows > kManyRows) {
+    join(attn_join_rows_kernel<D, KV>, kDecodeThreads / (D / 4));
+  } else {
+    if constexpr (kManyRows > kFewRows) join(attn_join_kernel<D, KV, 64>, kDecodeThreads / 64);
+  }
   return eldr_host::launch_status();
 }
 

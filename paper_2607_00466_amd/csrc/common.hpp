@@ -13,6 +13,7 @@ constexpr int kWave = 64;    // CDNA wavefront width
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 // Native 128-bit vector (HIP's uint4 is a struct the optimiser cannot always
 // keep in registers when it is copied whole).
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
