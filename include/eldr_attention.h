@@ -39,7 +39,10 @@
  * multiple of 16, lets keys and values, or layers, interleave in one allocation).  Offsets are
  * computed in 64 bits.  kv_type MOE_KV_BF16: values are bf16.  MOE_KV_FP8:
  * values are OCP e4m3 codes that stand for code * scale[h], with k_scale and
- * v_scale [Hkv] fp32 device arrays (NULL: all 1); ignored for bf16.
+ * v_scale [Hkv] fp32 device arrays (NULL: all 1); ignored for bf16.  A third type,
+ * MOE_KV_INT8, has a scale for each page and kv head: eldr_kv_cache.h describes it and
+ * has the call that fills it; of the calls below moe_attn_decode reads it, the others
+ * return MOE_ERR_UNSUPPORTED.
  *
  * Token slot j of request r lies in page block_table[r, j / block_size] at
  * offset j % block_size.  A slot whose page is outside [0, num_blocks) is

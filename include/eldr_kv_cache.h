@@ -86,8 +86,9 @@ int moe_kv_append_norm(const void* q, const void* k, const void* v, int64_t q_st
  *
  * What is not stored: tokens past slot N, and those whose page is absent.  Tokens
  * of no request (padding behind query_start[R]) are dropped, and their rows of
- * q_out are left as they are.  Pages that receive tokens are distinct for
- * distinct requests.  Slots past the new tokens are left as they are.
+ * q_out are left as they are.  Pages that receive tokens are distinct: for
+ * distinct requests, and for distinct places of a request's row.  Slots past the new
+ * tokens are left as they are.
  */
 int moe_kv_append_int8(const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride,
                        int64_t v_stride, int32_t in_type, int32_t T, const int32_t* positions,

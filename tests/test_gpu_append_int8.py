@@ -196,3 +196,31 @@ def test_values_at_the_borders_between_codes(top):
     before = c.numpy()
     append_int8(r, c, [0, r.T], [[2, 0, 1]], [0])
     check_append_int8(r, c, before, [0, r.T], [[2, 0, 1]], [0])
+
+
+def test_a_hundred_thousand_tokens():
+    """More tokens than a 16-bit grid has, none of them normed or turned."""
+    T = 100_003
+    r = Rows(T, 1, 1, 64, 0, norms=False, seed=11, fp32=False)
+    c = Int8Cache(-(-(T + 5) // 16) + 1, 1, 16, 64, seed=12)
+    table = np.random.default_rng(0).permutation(c.nb)[None].astype(np.int32)
+    before = c.numpy()
+    append_int8(r, c, [0, T], table, [5])
+    check_append_int8(r, c, before, [0, T], table, [5])
+    assert torch.equal(bits(r.q_out), bits(r.q.contiguous()))
+
+
+def test_offsets_past_2_to_31():
+    """Pages whose first code lies past 2^31, where the cache is 2.3 GB."""
+    nb, Hkv, bs, D = 35_200, 4, 128, 128
+    r, c = Rows(300, 4, Hkv, D, 64, seed=13), Int8Cache(4, Hkv, bs, D, seed=14)
+    k, v = (torch.empty((nb, Hkv, bs, D), dtype=torch.int8, device="cuda") for _ in "kv")
+    ks, vs = (torch.empty((nb, Hkv), device="cuda") for _ in "kv")
+    first = nb - c.nb
+    k[first:], v[first:], ks[first:], vs[first:] = c.k, c.v, c.k_scale, c.v_scale
+    table = np.array([[2, 0, 3]], np.int32)
+    append_int8(r, c, [0, 300], table, [50])
+    B.moe_kv_append_int8(r.q, r.k, r.v, r.positions, r.axis, r.cos, r.sin, i32([0, 300]), i32(table + first), i32([50]),
+                         B.attn_dims(1, 4, Hkv, D, bs, 3, nb, torch.int8), r.q_out, k, v, ks, vs, r.q_norm, r.k_norm)
+    for big, small in ((k, c.k), (v, c.v), (ks, c.k_scale), (vs, c.v_scale)):
+        assert torch.equal(big[first:], small)

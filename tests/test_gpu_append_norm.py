@@ -134,6 +134,19 @@ def test_rows_that_are_zero_infinite_or_nan():
     assert (r.q_out.float().cpu()[0] == 0).all()
 
 
+def test_on_a_side_stream():
+    a, b = Rows(40, 8, 2, 128, 64, seed=10), Rows(40, 8, 2, 128, 64, seed=10)
+    ka, va, _ = call(a, 16)
+    nb, d = 5, B.attn_dims(0, 8, 2, 128, 16, 1, 5)
+    slots = i32(np.random.default_rng(3).permutation(nb * 16)[:40])
+    k, v = (torch.full((nb, 2, 16, 128), 3.0, device="cuda").bfloat16() for _ in "kv")
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    B.moe_kv_append_norm(b.q, b.k, b.v, b.positions, b.axis, b.cos, b.sin, slots, d, b.q_out, k, v, b.q_norm, b.k_norm, stream=s)
+    s.synchronize()
+    assert torch.equal(bits(k), bits(ka)) and torch.equal(bits(v), bits(va)) and torch.equal(bits(a.q_out), bits(b.q_out))
+
+
 def test_captured_and_replayed():
     r = Rows(9, 8, 2, 128, 128, seed=9)
     ref = [call(r, 16, eps=1e-5)[0].clone(), r.q_out.clone()]

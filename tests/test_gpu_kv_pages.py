@@ -160,3 +160,64 @@ def test_replayed():
         np.testing.assert_array_equal(out.cpu().numpy(), want_out)
         np.testing.assert_array_equal(n.cpu().numpy(), want_n)
         same(pool, want)
+
+
+def test_on_side_streams():
+    """Each call on a stream of its own, nothing waiting between them."""
+    pools = [Pool(4, 30, 2, 16, 128, "int8", seed=i) for i in range(2)]
+    table, lens = np.array([[2, 3], [4, 5], [-1, -1], [-1, -1]], np.int32), np.array([20, 31, 0, 0])
+    remap = np.full(30, -1)
+    remap[[2, 3, 20, 25]] = [2, 3, 0, 1]
+    before = [p.numpy() for p in pools]
+    args = i32([0, 1]), i32([2, 3]), i32([8, 9]), i32(table), i32(lens)
+    old, out, r = i32([[2, 20], [25, 3]]), torch.zeros((2, 2), dtype=torch.int32, device="cuda"), i32(remap)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in pools]
+    B.moe_kv_fork(*args, pools[0].dims(4, 2), *pools[0].args(), stream=streams[0])
+    B.moe_kv_compact(r, old, out, pools[1].dims(2, 2), *pools[1].args(), stream=streams[1])
+    for s in streams:
+        s.synchronize()
+    want_t, want_n, *want = K.fork([0, 1], [2, 3], [8, 9], table, lens, *before[0])
+    np.testing.assert_array_equal(args[3].cpu().numpy(), want_t)
+    same(pools[0], want)
+    want_out, *want = K.compact(remap, np.array([[2, 20], [25, 3]]), *before[1])
+    np.testing.assert_array_equal(out.cpu().numpy(), want_out)
+    same(pools[1], want)
+
+
+def test_no_layer_and_no_page():
+    """The tables alone; and a cache without a page, of which everything is absent."""
+    for layers, nb in ((0, 6), (2, 0)):
+        d = B.attn_dims(2, 2, 2, 64, 16, 2, nb, torch.bfloat16)
+        k = torch.zeros((layers, nb, 2, 16, 64), dtype=torch.bfloat16, device="cuda")
+        t, n = i32([[4, 3], [-1, -1]]), i32([20, 0])
+        B.moe_kv_fork(i32([0]), i32([1]), i32([5]), t, n, d, k, k.clone())
+        assert t.tolist() == [[4, 3], [4, 5 if nb else -1]] and n.tolist() == [20, 20]
+        B.moe_kv_compact(i32([-1, -1, -1, 0, 1, 2][:nb]), t, t, d, k, k.clone())
+        assert t.tolist() == ([[1, 0], [1, 2]] if nb else [[-1, -1], [-1, -1]])
+
+
+def test_offsets_past_2_to_31():
+    """A page of the last of eight layers, past 2^31 codes: everything else stays."""
+    layers, nb, Hkv, bs, D = 8, 36_000, 4, 16, 128
+    caches = [torch.randint(-128, 128, (layers, nb, Hkv, bs, D), dtype=torch.int8, device="cuda") for _ in "kv"]
+    scales = [torch.rand((layers, nb, Hkv), device="cuda") for _ in "kv"]
+    was = [x.clone() for x in caches + scales]
+    d = B.attn_dims(2, 4, Hkv, D, bs, 2, nb, torch.int8)
+    remap = torch.full((nb,), -1, dtype=torch.int32, device="cuda")
+    remap[nb - 1], remap[7], remap[100] = nb - 2, 7, nb - 3
+    t = i32([[nb - 1, 7], [100, -1]])
+    B.moe_kv_compact(remap, t, t, d, *caches, *scales)
+    assert t.tolist() == [[nb - 2, 7], [nb - 3, -1]]
+    for x, w in zip(caches + scales, was):
+        w[:, nb - 2], w[:, nb - 3] = w[:, nb - 1].clone(), w[:, 100].clone()
+        assert torch.equal(x, w)
+    n = i32([21, 0])
+    B.moe_kv_fork(i32([0]), i32([1]), i32([nb - 5]), t, n, d, *caches, *scales)
+    assert t.tolist() == [[nb - 2, 7], [nb - 2, nb - 5]] and n.tolist() == [21, 21]
+    for x, w in zip(caches, was):
+        w[:, nb - 5, :, :5] = w[:, 7, :, :5].clone()
+        assert torch.equal(x, w)
+    for x, w in zip(scales, was[2:]):
+        w[:, nb - 5] = w[:, 7].clone()
+        assert torch.equal(x, w)
