@@ -22,6 +22,18 @@
 // 48 us (208 MB, 61% of the read's rate).  Dealing the units to waves in place of workgroups (no merge
 // in LDS, four times the parts) measured 2 to 8% slower.
 //
+// Pages of 8-bit integers: codes become bf16 exactly (a conversion each, its upper
+// half kept), a page's key scale multiplies the tile's scores where scale and units
+// already do, its value scale the tile's weights before they are split, so neither
+// costs a product over D.  A lane loads one of a step's four scales.  Measured: 128 of up
+// to 8000 (552 MB) 98 us, 64 of 16384 (1.1 GB) 168, 2 near 131,000 (268 MB) 46, within 1
+// to 4% of fp8 at every shape tried.  No gain came of more workgroups (768: 103.5 -> 106
+// us in the first case, 1024: 109), of a wave's next step asked for before this one is
+// worked on (237 registers; within 1%) and of the next segment's first step asked for
+// before the merge (within 2%, both ways): what is left is start and plan (5 us of every
+// call), the join and the ends of segments (128 of 4096, one to a workgroup, run at 6.2
+// TB/s; of 17 to 8000 at 5.6).
+//
 // The four waves of a workgroup take turns at a segment's 32-slot steps and
 // meet in LDS at its end.  A segment that is a request's whole context gives
 // the output; the others leave sums that attn_join adds up.

@@ -13,6 +13,15 @@
 // a head a thread), 64 tokens in bf16 3.7 us; 1001 tokens of 80 heads of 64 to fp8
 // 7.3 us where the bytes take 4: all 5008 waves are resident at once, so the small
 // batch's latency is there beside the bytes.
+//
+// Norms add a sum over the lanes of a row (in 64 bits: append_rows.hpp) and 16 weights
+// in registers, read again only where a thread goes from queries to keys.  They cost
+// waves (five or six a SIMD in place of eight), not bytes: 4096 tokens of 40 heads of 128 in bf16 18.5 us
+// (4.6 TB/s), 4097 from fp32 to fp8 30 to 32 where the bytes take 25, 64 tokens 3.6 to 4.
+// Six waves by the launch bound (five with fp8's divisions, which spill at six) gave 2 to
+// 4%; the next head's row asked for early costs more waves than it gains (18.9 -> 20.0).
+// Queries written past the caches take 4 us off the 4096, and give whoever reads them
+// next 7 more (29.0 -> 32.2 with a copy of them behind), so they are not.
 #include "append_rows.hpp"
 #include "eldr_kv_cache.h"
 
