@@ -79,7 +79,7 @@ extern "C" {
 /* What the caches hold. */
 #define MOE_KV_BF16 0
 #define MOE_KV_FP8 1
-#define MOE_KV_INT8 3 /* a scale for each page and kv head: eldr_kv_cache.h */
+#define MOE_KV_INT8 3 /* (2 is no type) a scale for each page and kv head: eldr_kv_cache.h */
 
 /* What moe_kv_append's q, k and v are. */
 #define MOE_IN_BF16 0

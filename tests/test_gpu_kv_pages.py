@@ -221,3 +221,12 @@ def test_offsets_past_2_to_31():
     for x, w in zip(scales, was[2:]):
         w[:, nb - 5] = w[:, 7].clone()
         assert torch.equal(x, w)
+
+
+def test_a_tensor_on_another_device_is_named(monkeypatch):
+    """Kernels run on the current device: a cache elsewhere is refused before the launch."""
+    pool = Pool(1, 4, 2, 16, 64, "bf16", flat=True)
+    t = i32([[0, 1]])
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(ValueError, match="k_cache: is on cuda:0, and the current device is cuda:1"):
+        B.moe_kv_compact(i32([0, 1, 2, 3]), t, t, pool.dims(1, 2), *pool.args())
