@@ -28,6 +28,12 @@ __device__ __forceinline__ f32x4 mfma16x16x32(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
 }
 
+// Workgroups of up to 256 threads by number, kGridRow to a row of the grid
+// (eldr_host::grid_of): HIP counts a row's threads in 32 bits, and a launch of a longer
+// row leaves out the rest without an error.  The last row is launched whole.
+constexpr uint32_t kGridRow = 1u << 23;
+__device__ __forceinline__ uint32_t grid_block() { return blockIdx.y * kGridRow + blockIdx.x; }
+
 __device__ __forceinline__ float silu(float z) { return z / (1.0f + __expf(-z)); }
 
 }  // namespace eldr
@@ -47,6 +53,12 @@ inline int check_dims(const moe_dims& d) {
     return MOE_ERR_UNSUPPORTED;
   if (d.H % 32 != 0 || d.I % 32 != 0) return MOE_ERR_UNSUPPORTED;
   return MOE_OK;
+}
+
+// The grid of so many workgroups, at most 2^31 - 1 of them.
+inline dim3 grid_of(int64_t blocks) {
+  const int64_t rows = (blocks + eldr::kGridRow - 1) / eldr::kGridRow;
+  return rows <= 1 ? dim3((unsigned)blocks) : dim3(eldr::kGridRow, (unsigned)rows);
 }
 
 inline int launch_status() {

@@ -234,9 +234,9 @@ __device__ __forceinline__ void quantise_tile(const QuantArgs& a, const Pages& p
 
 // A wave's (or workgroup's) tile: which page and rows it is.
 template <typename In, int D, bool INTERLEAVED, int WAVES>
-__device__ __forceinline__ void quantise_page(const QuantArgs& a, const Pages& pg, uint32_t* tops) {
+__device__ __forceinline__ void quantise_page(const QuantArgs& a, const Pages& pg, int block, uint32_t* tops) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int tile = WAVES == 1 ? blockIdx.x * (kQuantThreads / kWave) + wave : blockIdx.x;
+  const int tile = WAVES == 1 ? block * (kQuantThreads / kWave) + wave : block;
   if (tile >= a.tiles) return;
   const int kinds = 2 * pg.Hkv, u = tile / kinds;
   // (a decode batch: request u's own token)
@@ -257,8 +257,9 @@ __device__ __forceinline__ void quantise_page(const QuantArgs& a, const Pages& p
 
 // Queries: as in moe_kv_append, several heads a thread with the angles it has read.
 template <typename In, int D, bool INTERLEAVED>
-__device__ __forceinline__ void turn_queries(const QuantArgs& a, int block) {
+__device__ __forceinline__ void turn_queries(const QuantArgs& a, uint32_t block) {
   constexpr int kLanes = D / 16;
+  if (!a.q_out) return;  // (the rest of a grid's last row)
   const int64_t id = (int64_t)block * kQuantThreads + threadIdx.x, th = id / kLanes;
   const int chunk = (int)(id % kLanes), t = (int)(th / a.q_lanes);
   if (t >= min(a.turns.T, a.start_of(a.R)) || t < a.start_of(0)) return;
@@ -290,16 +291,17 @@ __device__ __forceinline__ void turn_queries(const QuantArgs& a, int block) {
 template <typename In, int D, bool INTERLEAVED, int WAVES>
 __global__ __launch_bounds__(kQuantThreads) void kv_append_int8_kernel(QuantArgs a, Pages pg) {
   __shared__ uint32_t tops[kQuantThreads / kWave];
-  if ((int)blockIdx.x < a.tile_blocks) quantise_page<In, D, INTERLEAVED, WAVES>(a, pg, tops);
-  else turn_queries<In, D, INTERLEAVED>(a, blockIdx.x - a.tile_blocks);
+  const uint32_t block = grid_block();
+  if (block < (uint32_t)a.tile_blocks) quantise_page<In, D, INTERLEAVED, WAVES>(a, pg, (int)block, tops);
+  else turn_queries<In, D, INTERLEAVED>(a, block - a.tile_blocks);
 }
 
 template <typename In, int D>
-void launch_int8(const QuantArgs& a, const Pages& pg, bool interleaved, unsigned blocks, hipStream_t s) {
+void launch_int8(const QuantArgs& a, const Pages& pg, bool interleaved, dim3 grid, hipStream_t s) {
   const bool wave = pg.shift == 4;
   const auto kernel = wave ? interleaved ? kv_append_int8_kernel<In, D, true, 1> : kv_append_int8_kernel<In, D, false, 1>
                            : interleaved ? kv_append_int8_kernel<In, D, true, 4> : kv_append_int8_kernel<In, D, false, 4>;
-  hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kQuantThreads), 0, s, a, pg);
+  hipLaunchKernelGGL(kernel, grid, dim3(kQuantThreads), 0, s, a, pg);
 }
 
 }  // namespace eldr
@@ -357,17 +359,17 @@ extern "C" int moe_kv_append_int8(const void* q, const void* k, const void* v, i
   if (tiles > 0x7fffffffLL - kWaves || tile_blocks + q_blocks > 0x7fffffffLL) return MOE_ERR_UNSUPPORTED;
   if (tile_blocks + q_blocks == 0) return MOE_OK;
   a.tiles = (int32_t)tiles, a.tile_blocks = (int32_t)tile_blocks;
-  const unsigned blocks = (unsigned)(tile_blocks + q_blocks);
+  const dim3 grid = grid_of(tile_blocks + q_blocks);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const bool inter = interleaved != 0;
   if (in_type == MOE_IN_FP32) {
-    if (d.D == 64) eldr::launch_int8<float, 64>(a, pg, inter, blocks, s);
-    else if (d.D == 128) eldr::launch_int8<float, 128>(a, pg, inter, blocks, s);
-    else eldr::launch_int8<float, 256>(a, pg, inter, blocks, s);
+    if (d.D == 64) eldr::launch_int8<float, 64>(a, pg, inter, grid, s);
+    else if (d.D == 128) eldr::launch_int8<float, 128>(a, pg, inter, grid, s);
+    else eldr::launch_int8<float, 256>(a, pg, inter, grid, s);
   } else {
-    if (d.D == 64) eldr::launch_int8<uint16_t, 64>(a, pg, inter, blocks, s);
-    else if (d.D == 128) eldr::launch_int8<uint16_t, 128>(a, pg, inter, blocks, s);
-    else eldr::launch_int8<uint16_t, 256>(a, pg, inter, blocks, s);
+    if (d.D == 64) eldr::launch_int8<uint16_t, 64>(a, pg, inter, grid, s);
+    else if (d.D == 128) eldr::launch_int8<uint16_t, 128>(a, pg, inter, grid, s);
+    else eldr::launch_int8<uint16_t, 256>(a, pg, inter, grid, s);
   }
   return launch_status();
 }

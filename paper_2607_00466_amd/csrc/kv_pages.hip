@@ -108,12 +108,13 @@ __global__ __launch_bounds__(kPageThreads) void kv_compact_kernel(const int32_t*
                                                                   int64_t entries, Pages pg, Layers c, int run, int runs, int share) {
   const int parts = runs * share;
   const int64_t moves = (int64_t)pg.num_blocks * parts;
-  if (blockIdx.x >= moves) {
-    const int64_t i = (blockIdx.x - moves) * kPageThreads + threadIdx.x;
+  const uint32_t block = grid_block();
+  if (block >= moves) {
+    const int64_t i = (block - moves) * kPageThreads + threadIdx.x;
     if (i < entries) table_out[i] = page_after(pg, remap, table[i]);
     return;
   }
-  const int b = (int)(blockIdx.x / (uint32_t)parts), part = (int)(blockIdx.x - (uint32_t)b * (uint32_t)parts);
+  const int b = (int)(block / (uint32_t)parts), part = (int)(block - (uint32_t)b * (uint32_t)parts);
   const int l0 = part / share * run, take = part % share;
   const int to = page_after(pg, remap, b);
   if (to < 0 || to == b) return;
@@ -197,7 +198,7 @@ extern "C" int moe_kv_compact(const int32_t* remap, const int32_t* block_table, 
   const int64_t blocks = (int64_t)d.num_blocks * deal.runs * deal.share + (entries + eldr::kPageThreads - 1) / eldr::kPageThreads;
   if (blocks > 0x7fffffffLL) return MOE_ERR_UNSUPPORTED;
   if (blocks == 0) return MOE_OK;
-  hipLaunchKernelGGL(eldr::kv_compact_kernel, dim3((unsigned)blocks), dim3(eldr::kPageThreads), 0, reinterpret_cast<hipStream_t>(stream), remap,
+  hipLaunchKernelGGL(eldr::kv_compact_kernel, grid_of(blocks), dim3(eldr::kPageThreads), 0, reinterpret_cast<hipStream_t>(stream), remap,
                      block_table, table_out, entries, pages_of(d, nullptr), c, deal.run, deal.runs, deal.share);
   return launch_status();
 }
