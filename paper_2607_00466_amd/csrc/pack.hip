@@ -26,7 +26,7 @@ __global__ __launch_bounds__(256) void pack_band_kernel(const u32x4* __restrict_
                                                         const u32x4* __restrict__ b,
                                                         int64_t pieces, int R, int K, int up,
                                                         u32x4* __restrict__ dst) {
-  const int64_t p = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t p = (int64_t)grid_block() * 256 + threadIdx.x;
   if (p >= pieces) return;
   const int lane = (int)(p & 63);
   const int64_t frag = p >> 6;
@@ -63,7 +63,7 @@ static int pack_band(const uint16_t* a, const uint16_t* b, int32_t E, int32_t R,
   if (a == dst || b == dst) return MOE_ERR_INVALID;
   const int64_t blocks = (pieces + 255) / 256;
   if (blocks > 0x7fffffffLL) return MOE_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL(pack_band_kernel, dim3((unsigned)blocks), dim3(256), 0,
+  hipLaunchKernelGGL(pack_band_kernel, grid_of(blocks), dim3(256), 0,
                      reinterpret_cast<hipStream_t>(stream), reinterpret_cast<const u32x4*>(a),
                      reinterpret_cast<const u32x4*>(b), pieces, R, K, up,
                      reinterpret_cast<u32x4*>(dst));
@@ -106,7 +106,7 @@ __global__ __launch_bounds__(256) void pack_mxfp4_kernel(
     const uint32_t* __restrict__ ca, const uint32_t* __restrict__ cb,
     const uint8_t* __restrict__ sa, const uint8_t* __restrict__ sb, int64_t pieces, int R, int K,
     int band_rows, u32x4* __restrict__ dq, uint32_t* __restrict__ ds) {
-  const int64_t p = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t p = (int64_t)grid_block() * 256 + threadIdx.x;
   if (p >= pieces) return;
   const int lane = (int)(p & 63);
   const int64_t q = p >> 6;  // (slot, wave band) unit in packed order
@@ -162,7 +162,7 @@ int pack_mxfp4(const uint8_t* ca, const uint8_t* sa, const uint8_t* cb, const ui
   if (codes == ca || codes == cb || scales == sa || scales == sb) return MOE_ERR_INVALID;
   const int64_t blocks = (pieces + 255) / 256;
   if (blocks > 0x7fffffffLL) return MOE_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL(eldr::pack_mxfp4_kernel, dim3((unsigned)blocks), dim3(256), 0,
+  hipLaunchKernelGGL(eldr::pack_mxfp4_kernel, grid_of(blocks), dim3(256), 0,
                      reinterpret_cast<hipStream_t>(stream), reinterpret_cast<const uint32_t*>(ca),
                      reinterpret_cast<const uint32_t*>(cb), sa, sb, pieces, R, K, band_rows,
                      reinterpret_cast<eldr::u32x4*>(codes), reinterpret_cast<uint32_t*>(scales));

@@ -40,7 +40,7 @@ __global__ __launch_bounds__(kSigThreads) void sig_capture_kernel(
     sum[i] = 0u;
   }
   __syncthreads();
-  const int64_t p = (int64_t)blockIdx.x * kSigThreads + threadIdx.x;  // (l * T + t) * K + j
+  const int64_t p = (int64_t)grid_block() * kSigThreads + threadIdx.x;  // (l * T + t) * K + j
   bool bad = false;
   if (p < picks) {
     const int64_t lt = p / K;
@@ -202,7 +202,7 @@ extern "C" int moe_sig_capture(const int32_t* ids, const int32_t* token_block, i
     return MOE_ERR_UNSUPPORTED;
   const int64_t blocks = (picks + eldr::kSigThreads - 1) / eldr::kSigThreads;
   if (blocks > 0x7fffffffLL) return MOE_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL(eldr::sig_capture_kernel, dim3((unsigned)blocks), dim3(eldr::kSigThreads), 0,
+  hipLaunchKernelGGL(eldr::sig_capture_kernel, grid_of(blocks), dim3(eldr::kSigThreads), 0,
                      reinterpret_cast<hipStream_t>(stream), ids, token_block, picks, T, K, layer0,
                      L, E, num_blocks, reinterpret_cast<uint32_t*>(sig), rejected);
   return launch_status();

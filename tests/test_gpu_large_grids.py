@@ -69,3 +69,42 @@ def test_append_a_million_tokens_of_many_heads(queries):
     if queries:
         for first in rows.values():
             assert torch.equal(q_out[first:first + bs], x[first:first + bs])
+
+
+def test_capture_of_many_picks():
+    """2^32 + 2^23 picks, of which two tokens' are in a block."""
+    layers, T, K, E = 513, 1 << 20, 8, 32
+    ids = torch.empty((layers, T, K), dtype=torch.int32, device="cuda")
+    block = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    few = torch.randint(0, E, (layers, 2, K), dtype=torch.int32, device="cuda")
+    tokens, blocks = [3, T - 1], i32([2, 0])
+    ids[:, tokens], block[tokens] = few, blocks
+    L = 516
+    got, want = (torch.zeros((3, L, E), dtype=torch.int8, device="cuda") for _ in "gw")
+    B.moe_sig_capture(ids, block, 2, L, E, got)
+    B.moe_sig_capture(few, blocks, 2, L, E, want)
+    assert torch.equal(got, want) and int(want.sum()) == 2 * layers * K
+
+
+def test_pack_large_experts():
+    """A layer's up projections of 2^35 values and more: the last expert's as when it is
+    packed alone."""
+    E, I, H = 129, 8192, 16384
+    w = torch.empty((E, I, H), dtype=torch.bfloat16, device="cuda")  # w1 and w3 alike
+    w[[0, E - 1]] = torch.randint(-2 ** 15, 2 ** 15, (2, I, H), dtype=torch.int16, device="cuda").view(torch.bfloat16)
+    got = B.moe_pack_up_weights(w, w).view(torch.int16)
+    for e in (0, E - 1):
+        assert torch.equal(got[e:e + 1], B.moe_pack_up_weights(w[e:e + 1], w[e:e + 1]).view(torch.int16))
+
+
+def test_pack_large_mxfp4_experts():
+    E, I, H = 257, 16384, 16384
+    c = torch.empty((E, I, H // 2), dtype=torch.uint8, device="cuda")
+    s = torch.empty((E, I, H // 32), dtype=torch.uint8, device="cuda")
+    for t in (c, s):
+        t[[0, E - 1]] = torch.randint(0, 256, (2, *t.shape[1:]), dtype=torch.uint8, device="cuda")
+    got = [t.view(E, -1) for t in B.moe_pack_mxfp4_up((c, s), (c, s))]
+    for e in (0, E - 1):
+        one = c[e:e + 1], s[e:e + 1]
+        for a, b in zip(got, B.moe_pack_mxfp4_up(one, one)):
+            assert torch.equal(a[e], b)
