@@ -900,6 +900,8 @@ def _need_layers(k_cache, v_cache, k_scale, v_scale, d: AttnDims):
                 raise TypeError(f"{name}: expected a torch tensor")
             if t.dim() != 5:
                 raise ValueError(f"{name}: expected [num_blocks, Hkv, block_size, D] or [layers, ...] of it, got {tuple(t.shape)}")
+            if t.shape[0] > 1 and t.stride(0) == 0 and t.numel() > 0:  # (0 would stand for dense layers)
+                raise ValueError(f"{name}: an expanded tensor's layers are all the same one")
             if t.shape[0] > 0:
                 _need_cache_rows(t[0], name, d)
         layers, strides = k_cache.shape[0], k_cache.stride()

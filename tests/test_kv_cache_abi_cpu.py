@@ -209,3 +209,17 @@ def test_the_example_evicts_nothing_of_8_bit_integers():
         sizes = dict(R=4, groups=2, prefix=32, own=16, budget=64, steps=3, recent=4, int8=True) | bad
         with pytest.raises(ValueError, match="8-bit integers"):
             E.Worker(synth.SHAPES["tiny"], E.Heads(4, 2, 64), **sizes)
+
+
+@pytest.mark.parametrize("kv", [torch.bfloat16, torch.int8])
+def test_layers_that_are_one(lib, kv):
+    """An expanded cache has a layer stride of 0, which the library takes for dense layers
+    and would write past the one that is there."""
+    dims = d(kv=kv)
+    whole = torch.zeros((3, 64, 2, 16, 128), dtype=kv)
+    one = whole[:1].expand(3, -1, -1, -1, -1)
+    for k, v, name in ((one, one, "k_cache"), (one, whole, "k_cache")):
+        with pytest.raises(ValueError, match=f"{name}: an expanded tensor's layers are all the same one"):
+            B._need_layers(k, v, None, None, dims)
+    with pytest.raises(ValueError, match="must be a device tensor"):  # (one layer, expanded or not, has no stride)
+        B._need_layers(whole[:1].expand(1, -1, -1, -1, -1), whole[:1], None, None, dims)
