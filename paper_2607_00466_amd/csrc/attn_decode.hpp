@@ -408,9 +408,13 @@ __global__ __launch_bounds__(kDecodeThreads) void attn_join_kernel(DecodeArgs a,
       v[b] = *reinterpret_cast<const f32x4*>(from + 4 * at);
       ml[b] = *reinterpret_cast<const f32x4*>(from + D);
     }
+    // (selects: a branch a part costs 2 us of 16 where rows have 250)
 #pragma unroll
-    for (int b = 0; b < kBatch; ++b)
-      if (p0 + b * kSets < count) x.add(ml[b][0], ml[b][1], v[b]);
+    for (int b = 0; b < kBatch; ++b) {
+      const bool there = p0 + b * kSets < count;
+      const f32x4 none = {0.f, 0.f, 0.f, 0.f};
+      x.add(there ? ml[b][0] : -INFINITY, ml[b][1], there ? v[b] : none);
+    }
   }
   sums[set][at] = x.sum;
   if (at == 0) tops[set] = x.top, totals[set] = x.total;
