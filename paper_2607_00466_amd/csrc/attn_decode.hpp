@@ -39,6 +39,8 @@
 // the output; the others leave sums that attn_join adds up.
 #pragma once
 
+#include <algorithm>
+
 #include "attn_plan.hpp"
 #include "attn_shared.hpp"
 #include "attn_tile.hpp"
@@ -320,6 +322,21 @@ struct RowParts {
   const float *shared, *shared_rest, *own, *own_rest;  // (own_rest, shared_rest: of the row's place in a tile)
   int shared_parts, own_parts, shared_w0, own_w0;
   int hq, h;  // the row's query head and kv head
+  bool many;  // Lines::many of its request
+};
+
+// The two lines as they were dealt.
+template <int D>
+struct Lines {
+  Deal own, shared;
+  __device__ __forceinline__ Lines(const DecodeArgs& a, const Pages& pg, const int* plan)
+      : own(plan[a.gr.R] * pg.Hkv * a.head_tiles, decode_wgs(D)),
+        shared(plan[3 * a.gr.R + 1 + a.gr.n] * pg.Hkv, kSharedWgs) {}
+  // Whether a request's rows are in more than some 8 parts, of so many units.
+  __device__ __forceinline__ bool many(int own_units, int shared_units) const {
+    constexpr int kFew = 8;
+    return own_units > kFew * own.each || shared_units > kFew * shared.each;
+  }
 };
 
 template <int D>
@@ -330,22 +347,21 @@ __device__ __forceinline__ RowParts parts_of(const DecodeArgs& a, const Pages& p
   const int *reach = own + R + 1, *group = reach + R, *shared = group + R;
   const int r = q_row / a.Hq, hq = q_row - r * a.Hq, h = hq / a.G, i = hq - h * a.G;
   const int own_row = own[R], tiles = own[r + 1] - own[r], mine = reach[r];
+  const Lines<D> lines(a, pg, parts.plan);
   RowParts p{parts.shared + (int64_t)q_row * kPitch, parts.shared_rest, parts.own + (int64_t)q_row * kPitch,
-             parts.own_rest + (int64_t)(i % kRows) * kPitch, 0, 0, 0, 0, hq, h};
+             parts.own_rest + (int64_t)(i % kRows) * kPitch, 0, 0, 0, 0, hq, h, lines.many(tiles, tiles_of(0, mine))};
   if (mine > 0) {
     const int g = group[r];
     const int row = (r - max(a.gr.start[g], 0)) * a.G + i, per = tiles_of(0, mine);
     const int u0 = h * shared[n] + shared[g] + row / kTileRows * per;
-    const Deal deal(shared[n] * pg.Hkv, kSharedWgs);
-    p.shared_w0 = deal.owner(u0);
-    p.shared_parts = deal.owner(u0 + per - 1) - p.shared_w0 + 1;
+    p.shared_w0 = lines.shared.owner(u0);
+    p.shared_parts = lines.shared.owner(u0 + per - 1) - p.shared_w0 + 1;
     p.shared_rest += (int64_t)(row % kTileRows) * kPitch;
   }
   if (tiles > 0) {
-    const Deal deal(own_row * pg.Hkv * a.head_tiles, decode_wgs(D));
     const int u0 = (h * a.head_tiles + i / kRows) * own_row + own[r];
-    p.own_w0 = deal.owner(u0);
-    p.own_parts = deal.owner(u0 + tiles - 1) - p.own_w0 + 1;
+    p.own_w0 = lines.own.owner(u0);
+    p.own_parts = lines.own.owner(u0 + tiles - 1) - p.own_w0 + 1;
   }
   return p;
 }
@@ -381,19 +397,24 @@ __device__ __forceinline__ void write_row(const DecodeArgs& a, int q_row, int hq
   if (at == 0 && a.lse) a.lse[q_row] = end.lse;
 }
 
-// Adds up the parts of a row that has several, and writes a row that has none.  For
-// few rows, each of them in many parts: THREADS threads (256, or 64) take a row, sets
-// of D / 4 of them its parts in turn, four values each, and the sets meet in LDS.
+// LDS where the sets of threads that share a row meet.
+template <int D, int THREADS>
+struct JoinLds {
+  static constexpr int kSet = D / 4, kSets = THREADS / kSet, kRowsWg = kDecodeThreads / THREADS;
+  f32x4 sums[kRowsWg][kSets][kSet];
+  float tops[kRowsWg][kSets], totals[kRowsWg][kSets];
+};
+
+// Adds up the parts of a row that has several, and writes a row that has none: THREADS
+// threads (256, or 64) take it (none where !real), sets of D / 4 of them its parts in
+// turn, four values each, and the sets meet in LDS.
 template <int D, int KV, int THREADS>
-__global__ __launch_bounds__(kDecodeThreads) void attn_join_kernel(DecodeArgs a, Pages pg, Parts parts, int rows) {
-  constexpr int kSet = D / 4, kSets = THREADS / kSet, kRowsWg = kDecodeThreads / THREADS;
-  __shared__ f32x4 sums_of[kRowsWg][kSets][kSet];
-  __shared__ float tops_of[kRowsWg][kSets], totals_of[kRowsWg][kSets];
+__device__ __forceinline__ void join_row(const DecodeArgs& a, const Pages& pg, const Parts& parts, JoinLds<D, THREADS>& lds, int q_row,
+                                         bool real) {
+  constexpr int kSet = D / 4, kSets = THREADS / kSet;
   const int mine_row = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
-  const bool real = (int)blockIdx.x * kRowsWg + mine_row < rows;
-  const int q_row = real ? blockIdx.x * kRowsWg + mine_row : 0;
-  auto& sums = sums_of[mine_row];
-  auto &tops = tops_of[mine_row], &totals = totals_of[mine_row];
+  auto& sums = lds.sums[mine_row];
+  auto &tops = lds.tops[mine_row], &totals = lds.totals[mine_row];
   const RowParts r = parts_of<D>(a, pg, parts, q_row);
   const bool written = !real || (r.own_parts == 1 && r.shared_parts == 0);  // by attn_decode
   const int set = threadIdx.x % THREADS / kSet, at = threadIdx.x % kSet;
@@ -418,23 +439,61 @@ __global__ __launch_bounds__(kDecodeThreads) void attn_join_kernel(DecodeArgs a,
   }
   sums[set][at] = x.sum;
   if (at == 0) tops[set] = x.top, totals[set] = x.total;
-  __syncthreads();
+  if constexpr (THREADS == kWave) wave_handover();
+  else __syncthreads();
   if (written || set != 0) return;
 #pragma unroll
   for (int s = 1; s < kSets; ++s) x.add(tops[s], totals[s], sums[s][at]);
   write_row<D, KV>(a, q_row, r.hq, r.h, at, x);
 }
 
-// The same for many rows, of a few parts each: D / 4 threads take a row.  What finds
+// For few rows, each of them in many parts.
+template <int D, int KV, int THREADS>
+__global__ __launch_bounds__(kDecodeThreads) void attn_join_kernel(DecodeArgs a, Pages pg, Parts parts, int rows) {
+  __shared__ JoinLds<D, THREADS> lds;
+  const int q_row = blockIdx.x * (kDecodeThreads / THREADS) + __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
+  const bool real = q_row < rows;
+  join_row<D, KV, THREADS>(a, pg, parts, lds, real ? q_row : 0, real);
+}
+
+// The same for many rows: D / 4 threads take a row of a few parts.  What finds
 // a row's parts (eight divisions) is then a wave's work for up to four rows, where a
 // wave a row spent most of its time (16,384 rows of 64: 15.5 -> 8 us).  The parts are
-// added as kWave / kSet sets would.
+// added as kWave / kSet sets would, so that a row's bits are the same either way.
+//
+// Where D / 4 threads are a quarter of a wave, a row of many parts has half as many of
+// them in flight here as 64 threads would have.  Such rows are a wave's work each, in
+// further workgroups, which look at every request.  Measured (us, whole calls, 64 heads of
+// 64; 64 threads every row, D / 4 every row, this): over 1 kv head one request of 131,000
+// slots beside 31 of 100 51.8, 74.6, 52.7, over 8 70.3, 81.3, 70.9, beside 255 78.3, 86.6,
+// 80.2; 256 of up to 1500 81.5, 76.0, 77.6, behind 8 x 2048 101, 93, 95, 128 of up to 1000
+// 34.4, 31.5, 32.1.  (A list of such requests first: 1 us less where rows are short, 1 more
+// where all have many parts.)
+constexpr int kApartWgs = 1024;
 template <int D, int KV>
 __global__ __launch_bounds__(kDecodeThreads) void attn_join_rows_kernel(DecodeArgs a, Pages pg, Parts parts, int rows) {
-  constexpr int kSet = D / 4, kSets = kWave / kSet;
-  const int q_row = blockIdx.x * (kDecodeThreads / kSet) + threadIdx.x / kSet, at = threadIdx.x % kSet;
+  constexpr int kSet = D / 4, kSets = kWave / kSet, kRowsWg = kDecodeThreads / kSet;
+  constexpr bool kApart = kSets > 2;
+  if constexpr (kApart) {
+    const int wgs = (rows + kRowsWg - 1) / kRowsWg;
+    if ((int)blockIdx.x >= wgs) {
+      __shared__ JoinLds<D, kWave> lds;
+      const Lines<D> lines(a, pg, parts.plan);
+      const int *own = parts.plan, *reach = own + a.gr.R + 1;
+      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+      for (int row = ((int)blockIdx.x - wgs) * kDecodeWaves + wave; row < rows; row += kApartWgs * kDecodeWaves) {
+        const int r = row / a.Hq;
+        if (!lines.many(own[r + 1] - own[r], tiles_of(0, reach[r]))) continue;
+        join_row<D, KV, kWave>(a, pg, parts, lds, row, true);
+        wave_handover();  // (before the next row's sums)
+      }
+      return;
+    }
+  }
+  const int q_row = blockIdx.x * kRowsWg + threadIdx.x / kSet, at = threadIdx.x % kSet;
   if (q_row >= rows) return;
   const RowParts r = parts_of<D>(a, pg, parts, q_row);
+  if (kApart && r.many) return;
   if (r.own_parts == 1 && r.shared_parts == 0) return;  // written by attn_decode
   const int count = r.shared_parts + r.own_parts;
   constexpr int kBatch = 8;  // parts in flight
@@ -483,20 +542,23 @@ int launch_decode(const DecodeArgs& a, const Pages& pg, float* ws, hipStream_t s
   // Measured (us, whole calls; 256 threads a row, 64): 64 rows of 131,000 slots 51, 59;
   // 512 of 16,384 73, 74, and behind 8192 37, 43; 1024 of up to 8000 70, 69, and behind
   // 8192 40, 42; 2048 of up to 8000 138, 136; 8192 behind 2048 73, 54; 16,384 of up to
-  // 1500 92, 71.  D / 4 threads a row against 64: D = 64, 16,384 rows behind 8 x 2048 88.8,
-  // 95.7, of up to 1500 52.3, 57.0, 4096 of up to 700 16.1, 17.0, behind 8192 52.8, 52.8;
-  // D = 128, 8192 of up to 1500 49.7, 51.8, 4096 of up to 8000 103.4, 103.9, behind 4 x 2048
-  // 51.8, 49.8, 2048 behind 8192 51.5, 49.9; D = 256 the same.
+  // 1500 92, 71.  D / 4 threads a row (few parts) against 64, in
+  // fp8: D = 64, 16,384 rows behind 8 x 2048 75.2, 81.2, of up to 1500 47.0, 51.2, 4096 of
+  // up to 700 15.1, 16.3, behind 8192 48.8, 49.2; D = 128, 8192 of up to 1500 44.1, 46.1,
+  // behind 8 x 2048 71.5, 71.5, 5120 of which 32 of 131,000 72.2, 71.2, 4096 of up to 8000
+  // (8-bit integers) 101.5, 102.2, behind 4 x 2048 52.1, 49.7, 2048 behind 8192 (bf16) 48.2,
+  // 49.0; D = 256 the same.
   constexpr int64_t kFewRows = 1024, kManyRows = D == 64 ? kFewRows : 4096;
-  const auto join = [&](auto kernel, int rows_wg) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + rows_wg - 1) / rows_wg)), dim3(kDecodeThreads), 0, s, a, pg, parts, (int)rows);
+  const auto wgs = [&](int rows_wg) { return (unsigned)((rows + rows_wg - 1) / rows_wg); };
+  const auto join = [&](auto kernel, unsigned wgs) {
+    hipLaunchKernelGGL(kernel, dim3(wgs), dim3(kDecodeThreads), 0, s, a, pg, parts, (int)rows);
   };
   if (rows <= kFewRows) {
-    join(attn_join_kernel<D, KV, 256>, 1);
+    join(attn_join_kernel<D, KV, 256>, wgs(1));
   } else if (rows > kManyRows) {
-    join(attn_join_rows_kernel<D, KV>, kDecodeThreads / (D / 4));
+    join(attn_join_rows_kernel<D, KV>, wgs(kDecodeThreads / (D / 4)) + (D == 64 ? std::min(wgs(kDecodeWaves), (unsigned)kApartWgs) : 0));
   } else {
-    if constexpr (kManyRows > kFewRows) join(attn_join_kernel<D, KV, 64>, kDecodeThreads / 64);
+    if constexpr (kManyRows > kFewRows) join(attn_join_kernel<D, KV, 64>, wgs(kDecodeThreads / 64));
   }
   return eldr_host::launch_status();
 }

@@ -1,11 +1,12 @@
 """moe_attn_decode's joins: which kernel adds a row's parts up goes by how many rows there
-are (1024, and 4096 where D is 128 or 256).  Row counts around the limits, the last
-workgroup partly filled, rows without a part, with one, with a few and with many, of their
-own and of a prefix."""
+are (1024, and 4096 where D is 128 or 256) and, where D is 64, by how many parts a
+request's rows have.  Row counts around the limits, the last workgroup partly filled,
+rows without a part, with one, with a few and with many, of their own and of a prefix."""
 import numpy as np
 import pytest
 import torch
 
+from paper_2607_00466_amd import binding as B
 from tests import attention_util as U
 from tests.test_gpu_attention_int8 import Cache as Int8Cache
 
@@ -85,3 +86,25 @@ def test_the_bits_of_a_row_are_those_of_either_join(kind, D):
     got = U.run_decode(more, torch.cat([q, q[:1]]), check=False)
     assert torch.equal(got[0][:128], out) and torch.equal(got[1][:128], lse)
     assert (got[0][128] == 0).all() and torch.isinf(got[1][128]).all()
+
+
+def test_replayed_while_a_request_becomes_long():
+    """The rule is the device's: a captured step of short requests, one of which grows."""
+    c = U.Cache([5000] + [40] * 40, 2, 64, 16, seed=9)
+    q, d = U.queries(41, 32, 64), c.dims(32)
+    lens, ws = torch.zeros(41, dtype=torch.int32, device="cuda"), B.attn_workspace(d)
+    out, lse = torch.empty_like(q), torch.empty((41, 32), device="cuda")
+    go = lambda: B.moe_attn_decode(q, c.k, c.v, c.table, lens, d, out, lse, ws)  # noqa: E731
+    go()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        go()
+    for n in (0, 30, 900, 5000, 12):
+        c.lens_np = np.array([n] + [40] * 40)
+        c.lens.copy_(torch.tensor(c.lens_np))
+        lens.copy_(c.lens)
+        g.replay()
+        torch.cuda.synchronize()
+        want = U.run_decode(c, q)
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
