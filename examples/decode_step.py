@@ -16,7 +16,7 @@ Each step, all on one stream and without a host synchronisation:
   6. moe_kv_evict     requests over their budget lose their lightest tokens
 
 A cache of 8-bit integers has a scale for each page and does without 5 and 6, so the
-budget has to hold every step's token.
+budget has to hold every step's token, and does where none is given.
 
 Random weights and hidden states; the projections are torch's, everything else is
 the library's.
@@ -36,6 +36,7 @@ from paper_2607_00466_amd import binding as B  # noqa: E402
 from paper_2607_00466_amd import synth  # noqa: E402
 
 BLOCK = 16
+RECENT = 32  # tokens that are never evicted
 
 
 @dataclass
@@ -45,19 +46,23 @@ class Heads:
     D: int
 
 
+def check_sizes(groups, prefix, own, budget, steps, recent=RECENT, fp8=False, int8=False):
+    if prefix % BLOCK or budget < prefix + recent:
+        raise ValueError("the prefix is whole pages, and the budget holds it and the recent tokens")
+    if steps < 1 or own < 0 or groups < 1:
+        raise ValueError("a worker has a step to make, a group and no fewer than 0 tokens of its own a request")
+    if int8 and (fp8 or budget < prefix + own + steps):
+        raise ValueError("a cache of 8-bit integers is none of fp8, and nothing is evicted from it: the budget holds every token")
+
+
 class Worker:
     """One layer's weights, and the batch's cache: `groups` equal groups of requests,
     each behind `prefix` shared tokens and with `own` tokens of its own, with room
     for `steps` steps."""
 
     def __init__(self, shape: synth.LayerShape, heads: Heads, R: int, groups: int, prefix: int, own: int, budget: int,
-                 steps: int, recent: int = 32, fp8: bool = False, int8: bool = False, norm: bool = False, seed: int = 0):
-        if prefix % BLOCK or budget < prefix + recent:
-            raise ValueError("the prefix is whole pages, and the budget holds it and the recent tokens")
-        if steps < 1 or own < 0 or groups < 1:
-            raise ValueError("a worker has a step to make, a group and no fewer than 0 tokens of its own a request")
-        if int8 and (fp8 or budget < prefix + own + steps):
-            raise ValueError("a cache of 8-bit integers is none of fp8, and nothing is evicted from it: the budget holds every token")
+                 steps: int, recent: int = RECENT, fp8: bool = False, int8: bool = False, norm: bool = False, seed: int = 0):
+        check_sizes(groups, prefix, own, budget, steps, recent, fp8, int8)
         self.left = steps
         self.shape, self.heads, self.budget, self.recent = shape, heads, budget, recent
         gen = torch.Generator(device="cuda").manual_seed(seed)
@@ -185,7 +190,7 @@ class Worker:
         return x
 
 
-def main(argv=None):
+def arguments(argv=None):
     p = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     p.add_argument("--shape", default="qwen3_30b_a3b", choices=sorted(synth.SHAPES))
     p.add_argument("--heads", type=int, nargs=3, default=(32, 4, 128), metavar=("HQ", "HKV", "D"))
@@ -193,12 +198,19 @@ def main(argv=None):
     p.add_argument("--groups", type=int, default=1)
     p.add_argument("--prefix", type=int, default=2048)
     p.add_argument("--own", type=int, default=256)
-    p.add_argument("--budget", type=int, default=2304)
+    p.add_argument("--budget", type=int, help="default 2304; with --int8 every token of the run")
     p.add_argument("--steps", type=int, default=20)
     p.add_argument("--fp8", action="store_true")
     p.add_argument("--int8", action="store_true")
     p.add_argument("--norm", action="store_true")
     a = p.parse_args(argv)
+    if a.budget is None:
+        a.budget = a.prefix + max(a.own + a.steps, RECENT) if a.int8 else 2304
+    return a
+
+
+def main(argv=None):
+    a = arguments(argv)
     w = Worker(synth.SHAPES[a.shape], Heads(*a.heads), a.requests, a.groups, a.prefix, a.own, a.budget, a.steps, fp8=a.fp8,
                int8=a.int8, norm=a.norm)
     x = torch.randn((a.requests, w.shape.H), device="cuda")
