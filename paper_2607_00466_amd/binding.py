@@ -760,6 +760,15 @@ def _stream_here(stream, t: torch.Tensor, name: str) -> int:
     return _raw_stream(here) if stream is None and _raw_stream is not None else _stream(stream)
 
 
+def _stream_of(stream, t: torch.Tensor, name: str) -> int:
+    """_stream, which has to be of the device that t is on."""
+    if stream is None:
+        return _stream_here(None, t, name)
+    if t.device != stream.device:
+        raise ValueError(f"{name}: is on {t.device}, and the stream on {stream.device}")
+    return stream.cuda_stream
+
+
 def _need_rows(t: torch.Tensor, name: str, T: int, heads: int, D: int) -> int:
     """A [T, heads, D] tensor whose heads and values are contiguous; its token stride."""
     if isinstance(t, torch.Tensor) and t.is_cuda and t.shape == (T, heads, D):
@@ -838,7 +847,7 @@ def moe_kv_append(q, k, v, positions, pair_axis, cos, sin, slots, d: AttnDims, q
     _need_cache(k_cache, "k_cache", d)
     _need_cache(v_cache, "v_cache", d)
     status = load().moe_kv_append(*rows, slots.data_ptr(), d, _ptr(k_scale), _ptr(v_scale), pq_out, k_cache.data_ptr(),
-                                  v_cache.data_ptr(), _stream(stream))
+                                  v_cache.data_ptr(), _stream_of(stream, k_cache, "k_cache"))
     if status:
         _check("moe_kv_append", status)
 
@@ -991,7 +1000,7 @@ def moe_attn_decode(q, k_cache, v_cache, block_table, lens, d: AttnDims, out, ls
     _check("moe_attn_decode", load().moe_attn_decode(
         _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(lens), _ptr(group_start), _ptr(prefix_len),
         groups, _ptr(k_scale), _ptr(v_scale), _ptr(sinks), window, d.D ** -0.5 if scale is None else scale, d,
-        _ptr(out), _ptr(lse), _ptr(ws), ws_bytes, _stream(stream)))
+        _ptr(out), _ptr(lse), _ptr(ws), ws_bytes, _stream_of(stream, k_cache, "k_cache")))
 
 
 def moe_attn_weights(q, k_cache, block_table, lens, lse, d: AttnDims, weights_in, weights_out, group_start=None,
@@ -1011,7 +1020,7 @@ def moe_attn_weights(q, k_cache, block_table, lens, lse, d: AttnDims, weights_in
     _check("moe_attn_weights", load().moe_attn_weights(
         _ptr(q), _ptr(k_cache), _ptr(block_table), _ptr(lens), _ptr(group_start), _ptr(prefix_len), groups,
         _ptr(k_scale), d.D ** -0.5 if scale is None else scale, _ptr(lse), d, _ptr(weights_in), _ptr(weights_out),
-        _stream(stream)))
+        _stream_of(stream, k_cache, "k_cache")))
 
 
 def moe_kv_evict(weights, pos, lens, seen, block_table, d: AttnDims, budget: int, recent: int, k_cache, v_cache, src,
@@ -1035,7 +1044,7 @@ def moe_kv_evict(weights, pos, lens, seen, block_table, d: AttnDims, budget: int
     _need(pos_out, "pos_out", torch.int32, rows)
     _check("moe_kv_evict", load().moe_kv_evict(
         _ptr(weights), _ptr(pos), _ptr(lens), _ptr(seen), _ptr(protect), _ptr(block_table), d, budget, recent,
-        _ptr(k_cache), _ptr(v_cache), _ptr(src), _ptr(new_lens), _ptr(weights_out), _ptr(pos_out), _stream(stream)))
+        _ptr(k_cache), _ptr(v_cache), _ptr(src), _ptr(new_lens), _ptr(weights_out), _ptr(pos_out), _stream_of(stream, k_cache, "k_cache")))
 
 
 # ----------------------------------------------------------------------------- calibration
