@@ -18,7 +18,6 @@ library's entry points.  Shapes are those of the decode layers this repository n
 
 A cache of 8-bit integers is returned as its codes, whole numbers, with the scales beside them.
 """
-import functools
 import math
 import random
 
@@ -386,12 +385,14 @@ def _dims(s, kv):
     return B.attn_dims(s.get("R", 0), s.get("Hq", s["Hkv"]), s["Hkv"], s["D"], s["bs"], s.get("max_blocks", 1), s["num_blocks"], kv)
 
 
-@functools.lru_cache(maxsize=8)
-def _workspace(R, Hq, Hkv, D):
-    """The workspace that a program keeps for its batches of this shape."""
+def _workspace(s, d):
+    """The workspace that a program keeps for its batches of this shape: one a state, since
+    calls on two streams cannot share one, nor calls on two devices."""
     from paper_2607_00466_amd import binding as B
 
-    return B.attn_workspace(B.attn_dims(R, Hq, Hkv, D, 16, 1, 1))
+    if "ws" not in s:
+        s["ws"] = B.attn_workspace(d, s["q"].device)
+    return s["ws"]
 
 
 def _own_norm(s):
@@ -415,8 +416,9 @@ def _own_quantise(s):
 def _own_attend(s):
     from paper_2607_00466_amd import binding as B
 
-    B.moe_attn_decode(s["q"], s["k_cache"], s["v_cache"], s["block_table"], s["lens"], _dims(s, INT8), s["out"], s["lse"],
-                      _workspace(s["R"], s["Hq"], s["Hkv"], s["D"]), group_start=s["group_start"],
+    d = _dims(s, INT8)
+    B.moe_attn_decode(s["q"], s["k_cache"], s["v_cache"], s["block_table"], s["lens"], d, s["out"], s["lse"],
+                      _workspace(s, d), group_start=s["group_start"],
                       prefix_len=s["prefix_len"], k_scale=s["k_scale"], v_scale=s["v_scale"], sinks=s["sinks"],
                       window=s["window"])
     return s["out"], s["lse"]
