@@ -108,3 +108,13 @@ def test_replayed_while_a_request_becomes_long():
         torch.cuda.synchronize()
         want = U.run_decode(c, q)
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 7, 1), (128, 5, 1), (256, 4, 2)])
+@pytest.mark.parametrize("pairs", [True, False])
+def test_the_most_requests_and_groups(kind, D, Hq, Hkv, pairs):
+    """The largest plan beside what the kernels keep in LDS."""
+    lens = lengths(1024, D, 50)
+    shared = [(r, r + 2, 16) for r in range(0, 1024, 2)] if pairs else [(r, r + 1, 16) for r in range(1024)]
+    check(kind, lens, Hq, Hkv, D, shared, seed=D)
