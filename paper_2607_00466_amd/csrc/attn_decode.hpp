@@ -458,17 +458,15 @@ __global__ __launch_bounds__(kDecodeThreads) void attn_join_kernel(DecodeArgs a,
 
 // The same for many rows: D / 4 threads take a row of a few parts.  What finds
 // a row's parts (eight divisions) is then a wave's work for up to four rows, where a
-// wave a row spent most of its time (16,384 rows of 64: 15.5 -> 8 us).  The parts are
+// wave a row spent most of its time (16,384 rows of 64: 15.5 -> 7.6 us).  The parts are
 // added as kWave / kSet sets would, so that a row's bits are the same either way.
 //
-// Where D / 4 threads are a quarter of a wave, a row of many parts has half as many of
-// them in flight here as 64 threads would have.  Such rows are a wave's work each, in
-// further workgroups, which look at every request.  Measured (us, whole calls, 64 heads of
-// 64; 64 threads every row, D / 4 every row, this): over 1 kv head one request of 131,000
-// slots beside 31 of 100 51.8, 74.6, 52.7, over 8 70.3, 81.3, 70.9, beside 255 78.3, 86.6,
-// 80.2; 256 of up to 1500 81.5, 76.0, 77.6, behind 8 x 2048 101, 93, 95, 128 of up to 1000
-// 34.4, 31.5, 32.1.  (A list of such requests first: 1 us less where rows are short, 1 more
-// where all have many parts.)
+// Where D / 4 threads are a quarter of a wave, a row of many parts has few of them in
+// flight here.  Such rows are a wave's work each, in further workgroups, which look at
+// every request.  Measured (us, whole calls, 64 heads of 64 in bf16; 64 threads every row,
+// D / 4 every row, this): over 1 kv head one request of 131,000 slots beside 31 of 100 51.6,
+// 74.6, 52.5, over 8 70.8, 81.2, 70.9, beside 255 78.3, 86.8, 80.0; 256 of up to 1500 81.6,
+// 76.2, 76.7, behind 8 x 2048 101, 93, 94, 128 of up to 1000 34.3, 31.5, 31.5.
 constexpr int kApartWgs = 1024;
 template <int D, int KV>
 __global__ __launch_bounds__(kDecodeThreads) void attn_join_rows_kernel(DecodeArgs a, Pages pg, Parts parts, int rows) {
@@ -496,7 +494,9 @@ __global__ __launch_bounds__(kDecodeThreads) void attn_join_rows_kernel(DecodeAr
   if (kApart && r.many) return;
   if (r.own_parts == 1 && r.shared_parts == 0) return;  // written by attn_decode
   const int count = r.shared_parts + r.own_parts;
-  constexpr int kBatch = 8;  // parts in flight
+  // parts in flight (where D is 64, registers for six waves a SIMD in place of four: 16,384
+  // rows 8.2 -> 7.6 us)
+  constexpr int kBatch = kApart ? 4 : 8;
   RowSums x[kSets];
   for (int p0 = 0; p0 < count; p0 += kBatch) {
     f32x4 v[kBatch];
