@@ -755,7 +755,7 @@ def _need_scales(k_scale, v_scale, d: AttnDims) -> None:
 def _stream_here(stream, t: torch.Tensor, name: str) -> int:
     """_stream, of the current device, which t has to be on: kernels run there."""
     here = torch.cuda.current_device()
-    if t.device.index != here:
+    if t.get_device() != here:
         raise ValueError(f"{name}: is on {t.device}, and the current device is cuda:{here}")
     return _raw_stream(here) if stream is None and _raw_stream is not None else _stream(stream)
 
@@ -763,6 +763,9 @@ def _stream_here(stream, t: torch.Tensor, name: str) -> int:
 def _stream_of(stream, t: torch.Tensor, name: str) -> int:
     """_stream, which has to be of the device that t is on."""
     if stream is None:
+        here = torch.cuda.current_device()
+        if t.get_device() == here and _raw_stream is not None:
+            return _raw_stream(here)
         return _stream_here(None, t, name)
     if t.device != stream.device:
         raise ValueError(f"{name}: is on {t.device}, and the stream on {stream.device}")
