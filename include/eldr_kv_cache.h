@@ -80,8 +80,9 @@ int moe_kv_append_norm(const void* q, const void* k, const void* v, int64_t q_st
  * (Round to nearest even.  A scale grows by powers of two so that a held value
  * never ends up more than one step of the page's last scale off, however often
  * it grew.  127 scale is compared exactly: rounding may leave it below the value
- * that set the scale, and a later row as large then doubles it.)  Where a, or a held page's scale, is not finite, scale' is NaN: the
- * page and head stand for NaN, as a NaN stored in the other caches would.
+ * that set the scale, and a later row as large then doubles it.)  Where a, or a
+ * held page's scale, is not finite, scale' is NaN: the page and head stand for NaN,
+ * as a NaN stored in the other caches would.
  * Held slots of a page whose scale was 0 become codes of 0.
  *
  * What is not stored: tokens past slot N, and those whose page is absent.  Tokens

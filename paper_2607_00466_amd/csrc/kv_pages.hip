@@ -7,6 +7,11 @@
 // of a thread's in flight.  Measured: 64 forks in 48 layers (46 MB read and written)
 // 11.4 us, 32 requests' pages compacted in 48 layers (533 MB) 115 us, 4.6 TB/s of a
 // large copy's 4.74 to 4.93; 4 forks in one layer 3.4.
+//
+// Compaction has a workgroup for every page and run of layers, moving or not, which is
+// what a pool much larger than what moves costs: 32 pages of 4 x 16 x 128 in 8 bits out
+// of 100,000 32 us in one layer and 62 in 8, out of 130,000 in 48 layers (102 GB) 455 (a
+// copy of them: 11); 1000 of those 640 (332).
 #include <algorithm>
 
 #include "attn_common.hpp"
